@@ -33,6 +33,8 @@ struct AttnParams {
     unsigned page_mul;                  // division of a group of 16 tokens by the page size: page_of
     float scale2, v_scale;              // scale * k_scale * log2 e
     int window, sinks;
+    int parts;                          // parts that the contexts of all tiles together are cut into, per key head
+    float *part_o, *part_ml;            // workspace: unfinished rows
 };
 
 // Page (index in a row of the table) of the 16 tokens from 16 * group on: group / (page_size / 16), by multiplication.
@@ -48,29 +50,108 @@ __device__ __forceinline__ void request_of(const AttnParams &p, int b, int &firs
     seq = min(max(p.seq_len[b], 0), p.max_pages * p.page_size);
 }
 
-// Which request the x-th tile of kRows rows belongs to and which of its tiles it is, found by every wave for itself.
-__device__ __forceinline__ bool find_tile(const AttnParams &p, int x, int &b, int &tile)
+// The blocks that a span of rows at positions pmin .. pmax sees: `lead` blocks of the first tokens that stay visible, then those from
+// `start` on; `count` in all.
+struct Blocks {
+    int lead, start, count;
+    __device__ __forceinline__ int at(int i) const { return i < lead ? i : start + i - lead; }
+};
+__device__ __forceinline__ Blocks blocks_of(const AttnParams &p, int pmin, int pmax)
 {
-    const int lane = lane_id();
-    int before = 0;
-    for (int b0 = 0; b0 < p.B; b0 += kWave) {
-        int tiles = 0;
-        if (b0 + lane < p.B) {
+    Blocks s;
+    const int end = pmax >= 0 ? pmax / kBlock + 1 : 0;
+    s.start = p.window == 0 ? 0 : min(max(pmin - p.window + 1, 0) / kBlock, end);
+    s.lead = p.window == 0 ? 0 : min((p.sinks - 1 + kBlock) / kBlock, s.start);
+    s.count = s.lead + end - s.start;
+    return s;
+}
+
+// How the work is cut.  A tile's context is cut into parts of at most `chunk` blocks, so that few rows with long contexts fill the
+// chip as well: chunk follows from the work of the whole batch (all tiles' blocks over p.parts) and is the same for all, so no
+// part is longer than the average workgroup's share.  Request lengths are on the device only; every workgroup works out for
+// itself which part it is: one round trip for the lengths (at most four requests a thread), two sums over the workgroup.
+constexpr int kMinChunk = 4;
+constexpr int kWorkgroups = 512;       // workgroups that the chip holds at once: two of four waves on each of 256 CUs
+constexpr int kMaxPerThread = LYNX_MAX_REQUESTS / kAttnThreads;
+struct Found {
+    int b, tile, split, splits, item;       // item: index of the tile's first part among those of all tiles that are cut
+};
+struct FindShared {
+    float work[kAttnWaves];
+    int sum[2][kAttnWaves];
+    Found found;
+};
+// CUT: x counts the tiles that are cut, otherwise the parts of all tiles.
+template <bool CUT>
+__device__ __forceinline__ bool find_work(const AttnParams &p, int x, FindShared &sh, Found &f)
+{
+    const int lane = lane_id(), wv = wave_id();
+    const int per = (p.B + kAttnThreads - 1) / kAttnThreads, b0 = threadIdx.x * per;
+    int tiles[kMaxPerThread], blocks[kMaxPerThread];
+    float work = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kMaxPerThread; ++i) {
+        tiles[i] = blocks[i] = 0;
+        if (i < per && b0 + i < p.B) {
             int first, n, seq;
-            request_of(p, b0 + lane, first, n, seq);
-            tiles = (n * p.G + kRows - 1) / kRows;
+            request_of(p, b0 + i, first, n, seq);
+            tiles[i] = (n * p.G + kRows - 1) / kRows;
+            blocks[i] = blocks_of(p, max(seq - n, 0), seq - 1).count;
+            work += (float)tiles[i] * (float)blocks[i];
         }
-        const int sum = wave_prefix_sum_i32(tiles);
-        const unsigned long long own = __ballot(before + sum > x && before + sum - tiles <= x);
-        if (own) {
-            const int src = __ffsll((long long)own) - 1;
-            b = b0 + src;
-            tile = x - (before + __builtin_amdgcn_readlane(sum - tiles, src));
-            return true;
-        }
-        before += __builtin_amdgcn_readlane(sum, 63);
     }
-    return false;
+    work = wave_sum(work);
+    if (threadIdx.x == 0) sh.found.b = -1;
+    if (lane == 0) sh.work[wv] = work;
+    __syncthreads();
+    work = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kAttnWaves; ++w) work += sh.work[w];
+    // (a little more than the quotient: the sum is rounded, and there are no more than p.parts + tiles workgroups)
+    const int chunk = max(kMinChunk, (int)(work * 1.0001f / (float)p.parts) + 1);
+    int nx = 0, nc = 0;
+#pragma unroll
+    for (int i = 0; i < kMaxPerThread; ++i) {
+        blocks[i] = max((blocks[i] + chunk - 1) / chunk, 1);      // parts of each of its tiles
+        nx += CUT ? (blocks[i] > 1 ? tiles[i] : 0) : tiles[i] * blocks[i];
+        nc += blocks[i] > 1 ? tiles[i] * blocks[i] : 0;
+    }
+    int sx = wave_prefix_sum_i32(nx), sc = wave_prefix_sum_i32(nc);
+    if (lane == kWave - 1) {
+        sh.sum[0][wv] = sx;
+        sh.sum[1][wv] = sc;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kAttnWaves; ++w) {
+        sx += w < wv ? sh.sum[0][w] : 0;
+        sc += w < wv ? sh.sum[1][w] : 0;
+    }
+    sx -= nx;
+    sc -= nc;
+    // the requests of this thread one by one: does x fall into one of them
+#pragma unroll
+    for (int i = 0; i < kMaxPerThread; ++i) {
+        const int items = CUT ? (blocks[i] > 1 ? tiles[i] : 0) : tiles[i] * blocks[i], at = x - sx;
+        if (at >= 0 && at < items) {
+            const int tile = CUT ? at : at / blocks[i];
+            sh.found.tile = tile;
+            sh.found.split = CUT ? 0 : at - tile * blocks[i];
+            sh.found.splits = blocks[i];
+            sh.found.item = sc + tile * blocks[i];
+            sh.found.b = b0 + i;
+        }
+        sx += items;
+        sc += blocks[i] > 1 ? tiles[i] * blocks[i] : 0;
+    }
+    __syncthreads();
+    f = sh.found;
+    f.b = __builtin_amdgcn_readfirstlane(f.b);
+    f.tile = __builtin_amdgcn_readfirstlane(f.tile);
+    f.split = __builtin_amdgcn_readfirstlane(f.split);
+    f.splits = __builtin_amdgcn_readfirstlane(f.splits);
+    f.item = __builtin_amdgcn_readfirstlane(f.item);
+    return f.b >= 0;
 }
 
 // Join over the four lanes l, l ^ 16, l ^ 32, l ^ 48 that hold parts of one row.
@@ -237,23 +318,39 @@ __device__ __forceinline__ void load_queries(const uint16_t *row, bool real, bf1
     }
 }
 
-// One workgroup per (tile of 16 rows of a request, key head); the blocks of its context go round the four waves, whose parts
-// of the softmax are joined in LDS.
+// A finished row piece of D / 16 channels: out = o * v_scale / l.
+template <int D>
+__device__ __forceinline__ void write_out(const AttnParams &p, int t, int head, int c0, float m, float l, const float (&o)[D / 16])
+{
+    const float inv = l == 0.0f ? 0.0f : p.v_scale / l;
+    uint16_t *dst = p.out + (size_t)t * p.out_stride + (size_t)head * D + c0;
+    if (D == 128) {
+        *reinterpret_cast<uint4 *>(dst) = make_uint4(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv),
+                                                     pack_bf16(o[D / 16 - 4] * inv, o[D / 16 - 3] * inv), pack_bf16(o[D / 16 - 2] * inv, o[D / 16 - 1] * inv));
+    } else {
+        *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+    }
+    if (p.lse && c0 == 0) p.lse[(size_t)t * (p.KVH * p.G) + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+}
+
+// One workgroup per (part of the context of a tile of 16 rows of a request, key head); the blocks of the part go round the four
+// waves, whose parts of the softmax are joined in LDS.
 template <int D, bool F8>
 __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnParams p)
 {
+    __shared__ FindShared sh;
     __shared__ float sm[kAttnWaves][kRows], sl[kAttnWaves][kRows];
     __shared__ __align__(16) float so[kAttnWaves][kRows][D + 4];
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id()), h = blockIdx.y;
-    int b, tile;
-    if (!find_tile(p, blockIdx.x, b, tile)) return;
+    Found f;
+    if (!find_work<false>(p, blockIdx.x, sh, f)) return;
     int first, n, seq;
-    request_of(p, b, first, n, seq);
-    const int r = tile * kRows + (lane & 15), rows = n * p.G;
+    request_of(p, f.b, first, n, seq);
+    const int r = f.tile * kRows + (lane & 15), rows = n * p.G;
     const bool real = r < rows;
     const int tok = real ? r / p.G : 0;
     const int pos = real ? seq - n + tok : -1;
-    const int pmin = max(seq - n + tile * kRows / p.G, 0), pmax = seq - n + (min(tile * kRows + kRows, rows) - 1) / p.G;
+    const int pmin = max(seq - n + f.tile * kRows / p.G, 0), pmax = seq - n + (min(f.tile * kRows + kRows, rows) - 1) / p.G;
     bf16x8 q[D / 32];
     load_queries<D, F8>(p.q + (size_t)(first + tok) * p.q_stride + (size_t)(h * p.G + (real ? r % p.G : 0)) * D, real, q);
 
@@ -262,13 +359,11 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnParams p)
     s.l = 0.0f;
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) s.o[t] = {0.0f, 0.0f, 0.0f, 0.0f};
-    // blocks the rows see: those of the first tokens that stay visible, then those of the window
-    const int end = pmax >= 0 ? pmax / kBlock + 1 : 0;
-    const int start = p.window == 0 ? 0 : min(max(pmin - p.window + 1, 0) / kBlock, end);
-    const int lead = p.window == 0 ? 0 : min((p.sinks - 1 + kBlock) / kBlock, start);
-    const int32_t *row = p.table + (size_t)b * p.max_pages;
-    for (int i = wv; i < lead + end - start; i += kAttnWaves) {
-        const int blk = i < lead ? i : start + i - lead;
+    const Blocks blocks = blocks_of(p, pmin, pmax);
+    const int per = (blocks.count + f.splits - 1) / f.splits, i0 = f.split * per, i1 = min(i0 + per, blocks.count);
+    const int32_t *row = p.table + (size_t)f.b * p.max_pages;
+    for (int i = i0 + wv; i < i1; i += kAttnWaves) {
+        const int blk = blocks.at(i);
         const int32_t *pages = (blk + 1) * kBlock <= p.prefix_len ? p.prefix_table : row;
         for (int t = 0; t < kBlock; t += Step<D, F8>::TN) Step<D, F8>::run(p, pages, h, blk * kBlock + t, q, pos, pmin, pmax, s);
     }
@@ -281,7 +376,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnParams p)
     for (int t = 0; t < D / 16; ++t) *reinterpret_cast<f32x4 *>(&so[wv][lane & 15][t * 16 + (lane >> 4) * 4]) = s.o[t];
     __syncthreads();
     // 16 threads per row, D / 16 channels each
-    const int orow = threadIdx.x / kRows, c0 = threadIdx.x % kRows * (D / 16), ro = tile * kRows + orow;
+    const int orow = threadIdx.x / kRows, c0 = threadIdx.x % kRows * (D / 16), ro = f.tile * kRows + orow;
     if (ro >= rows) return;
     float m = sm[0][orow];
 #pragma unroll
@@ -291,21 +386,94 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnParams p)
     for (int i = 0; i < D / 16; ++i) o[i] = 0.0f;
 #pragma unroll
     for (int w = 0; w < kAttnWaves; ++w) {
-        const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[w][orow] - m);
-        l += f * sl[w][orow];
+        const float e = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[w][orow] - m);
+        l += e * sl[w][orow];
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) o[i] += f * so[w][orow][c0 + i];
+        for (int i = 0; i < D / 16; ++i) o[i] += e * so[w][orow][c0 + i];
     }
+    if (f.splits == 1) {
+        write_out<D>(p, first + ro / p.G, h * p.G + ro % p.G, c0, m, l, o);
+        return;
+    }
+    const size_t part = ((size_t)(f.item + f.split) * p.KVH + h) * kRows + orow;
+    float4 *dst = reinterpret_cast<float4 *>(p.part_o + part * D + c0);
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+    if (c0 == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * part) = make_float2(m, l);
+}
+
+// Joins the parts of a tile's rows.  Few rows with many parts each are the case that counts (one request alone: a few rows, dozens
+// of parts), so a tile's rows are spread over kJoinSlices workgroups, and the parts of a row over what is left of the
+// workgroup's D / 4-lane groups, which meet in LDS.
+constexpr int kJoinSlices = 4;
+template <int D>
+__global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p)
+{
+    constexpr int L = D / 4, NG = kAttnThreads / L;         // lanes of a group (4 channels each), groups
+    __shared__ FindShared sh;
+    __shared__ float sm[NG], sl[NG];
+    __shared__ __align__(16) float4 so[NG][L];
+    Found f;
+    if (!find_work<true>(p, blockIdx.x, sh, f)) return;
+    int first, n, seq;
+    request_of(p, f.b, first, n, seq);
+    const int h = blockIdx.y, slice = blockIdx.z, here = min(n * p.G - f.tile * kRows, kRows);    // the tile's rows
+    const int mine = (here - slice + kJoinSlices - 1) / kJoinSlices;                               // those of this workgroup
+    if (mine <= 0) return;
+    const int width = mine > 2 ? 4 : mine;                                                         // (a power of two)
+    const int grp = threadIdx.x / L, lane = threadIdx.x % L, k = grp % width, sub = grp / width;
+    const int orow = slice + k * kJoinSlices;
+    const bool real = k < mine;
+    const size_t part = ((size_t)f.item * p.KVH + h) * kRows + (real ? orow : slice), step = (size_t)p.KVH * kRows;
+    float m = -INFINITY, l = 0.0f;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int i = sub; i < f.splits; i += NG / width) {
+        const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * (part + i * step));
+        const f32x4 u = *reinterpret_cast<const f32x4 *>(p.part_o + (part + i * step) * D + 4 * lane);
+        const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.0f : top;
+        const float a = __builtin_amdgcn_exp2f(m - base), e = __builtin_amdgcn_exp2f(ml.x - base);
+        l = l * a + e * ml.y;
+        o = o * a + u * e;
+        m = top;
+    }
+    if (lane == 0) {
+        sm[grp] = m;
+        sl[grp] = l;
+    }
+    so[grp][lane] = make_float4(o[0], o[1], o[2], o[3]);
+    __syncthreads();
+    if (sub != 0 || !real) return;
+    for (int w = k + width; w < NG; w += width) {
+        const float4 u = so[w][lane];
+        const float top = fmaxf(m, sm[w]), base = top == -INFINITY ? 0.0f : top;
+        const float a = __builtin_amdgcn_exp2f(m - base), e = __builtin_amdgcn_exp2f(sm[w] - base);
+        l = l * a + e * sl[w];
+        o = o * a + f32x4{u.x, u.y, u.z, u.w} * e;
+        m = top;
+    }
+    const int ro = f.tile * kRows + orow, t = first + ro / p.G, head = h * p.G + ro % p.G;
     const float inv = l == 0.0f ? 0.0f : p.v_scale / l;
-    const int head = h * p.G + ro % p.G, t = first + ro / p.G;
-    uint16_t *dst = p.out + (size_t)t * p.out_stride + (size_t)head * D + c0;
-    if (D == 128) {
-        *reinterpret_cast<uint4 *>(dst) = make_uint4(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv),
-                                                     pack_bf16(o[D / 16 - 4] * inv, o[D / 16 - 3] * inv), pack_bf16(o[D / 16 - 2] * inv, o[D / 16 - 1] * inv));
-    } else {
-        *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
-    }
-    if (p.lse && c0 == 0) p.lse[(size_t)t * (p.KVH * p.G) + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+    *reinterpret_cast<uint2 *>(p.out + (size_t)t * p.out_stride + (size_t)head * D + 4 * lane) =
+        make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+    if (p.lse && lane == 0) p.lse[(size_t)t * (p.KVH * p.G) + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+}
+
+// What the workspace holds: rows of unfinished parts, and their maxima and sums.  A tile that is cut has more than `chunk` blocks, so its
+// parts are fewer than twice blocks / chunk, and all such parts fewer than twice p.parts; there are at most p.parts such tiles.
+struct AttnSpace {
+    int tiles, parts;
+    size_t ml_off, total;
+};
+static AttnSpace attention_space(int B, int T, int QH, int KVH, int D)
+{
+    AttnSpace w;
+    w.tiles = B + (int)((int64_t)T * (QH / KVH) / kRows);     // sum of ceil(rows / 16) over requests
+    w.parts = kWorkgroups / KVH > 0 ? kWorkgroups / KVH : 1;
+    const size_t rows = (size_t)2 * w.parts * KVH * kRows;
+    w.ml_off = align256(rows * D * 4);
+    w.total = w.ml_off + align256(rows * 8);
+    return w;
 }
 
 static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, const void *k_cache, const void *v_cache, int cache_format,
@@ -327,15 +495,18 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
     if (!block_table || !q_start || !seq_len || (prefix_len > 0 && !prefix_table) || !workspace)
         return fail(LYNX_ERR_INVALID_ARG, "%s: null pointer", who);
     if ((rc = check_rows(who, "q", q, q_stride, QH, D)) != LYNX_OK || (rc = check_rows(who, "out", out, out_stride, QH, D)) != LYNX_OK) return rc;
-    const int G = QH / KVH;
-    AttnParams p = {q, k_cache, v_cache, block_table, q_start, seq_len, prefix_table, out, lse, q_stride, out_stride, B, T, KVH, G,
+    if (((uintptr_t)workspace & 255) != 0) return fail(LYNX_ERR_INVALID_ARG, "%s: the workspace must start on 256 bytes", who);
+    const AttnSpace w = attention_space(B, T, QH, KVH, D);
+    AttnParams p = {q, k_cache, v_cache, block_table, q_start, seq_len, prefix_table, out, lse, q_stride, out_stride, B, T, KVH, QH / KVH,
                     num_pages, max_pages, page_size, prefix_len, page_multiplier(page_size), scale * k_scale * kLog2e, v_scale,
-                    window < kMaxContext ? window : 0, sinks < kMaxContext ? sinks : kMaxContext};   // (a window that long hides nothing)
+                    window < kMaxContext ? window : 0, sinks < kMaxContext ? sinks : kMaxContext,   // (a window that long hides nothing)
+                    w.parts, (float *)workspace, (float *)((char *)workspace + w.ml_off)};
     const bool f8 = cache_format == LYNX_CACHE_FP8;
-    const int tiles = B + (int)((int64_t)T * G / kRows);     // sum of ceil(rows / 16) over requests
     auto kernel = D == 128 ? (f8 ? attn_rows_kernel<128, true> : attn_rows_kernel<128, false>)
                            : (f8 ? attn_rows_kernel<64, true> : attn_rows_kernel<64, false>);
-    hipLaunchKernelGGL(kernel, dim3(tiles, KVH), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
+    const bool cut = max_pages * page_size > kMinChunk * kBlock;       // else no context is long enough
+    hipLaunchKernelGGL(kernel, dim3(w.tiles + (cut ? w.parts : 0), KVH), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
+    if (cut) hipLaunchKernelGGL((D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>), dim3(w.tiles < w.parts ? w.tiles : w.parts, KVH, kJoinSlices), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
     return check_launch(who);
 }
 
@@ -344,7 +515,7 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
 extern "C" size_t lynx_attention_workspace_bytes(int B, int T, int QH, int KVH, int D, int prefix_len)
 {
     if (B <= 0 || T < 0 || QH <= 0 || KVH <= 0 || D <= 0 || prefix_len < 0) return 0;
-    return 256;
+    return lynx::attention_space(B, T, QH, KVH, D).total;
 }
 
 extern "C" int lynx_attention(const uint16_t *q, int64_t q_stride, const void *k_cache, const void *v_cache, int cache_format,
