@@ -20,6 +20,7 @@ constexpr int kBlock = 64;              // tokens of a block: the unit in which 
 constexpr int kRows = 16;               // rows of a tile
 constexpr int kAttnThreads = 256;
 constexpr int kAttnWaves = kAttnThreads / kWave;
+constexpr int kWorkgroups = 512;       // workgroups that the chip holds at once: two of four waves on each of 256 CUs
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 struct AttnParams {
@@ -66,92 +67,83 @@ __device__ __forceinline__ Blocks blocks_of(const AttnParams &p, int pmin, int p
     return s;
 }
 
-// How the work is cut.  A tile's context is cut into parts of at most `chunk` blocks, so that few rows with long contexts fill the
-// chip as well: chunk follows from the work of the whole batch (all tiles' blocks over p.parts) and is the same for all, so no
-// part is longer than the average workgroup's share.  Request lengths are on the device only; every workgroup works out for
-// itself which part it is: one round trip for the lengths (at most four requests a thread), two sums over the workgroup.
-constexpr int kMinChunk = 4;
-constexpr int kWorkgroups = 512;       // workgroups that the chip holds at once: two of four waves on each of 256 CUs
+// How the work is cut.  The blocks of all tiles, one tile after the other, are one long line that is cut into equal lengths, one
+// for each workgroup that the chip holds at once: however ragged the contexts, all workgroups read the same amount (with whole tiles
+// dealt out, 64 requests of 500 to 12000 tokens took 100 us where the equal cut takes 71).  A tile that a cut goes through is
+// finished by attn_join_kernel.  Request lengths are on the device only: every workgroup sums them up for itself, one round trip
+// for the lengths (at most four requests a thread) and one scan.
+constexpr int kMinLength = 4;               // blocks: fewer are not worth a workgroup
 constexpr int kMaxPerThread = LYNX_MAX_REQUESTS / kAttnThreads;
-struct Found {
-    int b, tile, split, splits, item;       // item: index of the tile's first part among those of all tiles that are cut
+struct Line {
+    unsigned ends[LYNX_MAX_REQUESTS];       // where each request's blocks end on the line
+    unsigned long long what[LYNX_MAX_REQUESTS];   // each request's first row (17 bits), rows (17 bits) and length (30 bits)
+    unsigned sum[kAttnWaves];
 };
-struct FindShared {
-    float work[kAttnWaves];
-    int sum[2][kAttnWaves];
-    Found found;
-};
-// CUT: x counts the tiles that are cut, otherwise the parts of all tiles.
-template <bool CUT>
-__device__ __forceinline__ bool find_work(const AttnParams &p, int x, FindShared &sh, Found &f)
+// Blocks of each tile of a request: those that its last rows and its first see together, so no tile has more; one at least.
+__device__ __forceinline__ unsigned blocks_per_tile(const AttnParams &p, int n, int seq)
+{
+    return (unsigned)max(blocks_of(p, max(seq - n, 0), seq - 1).count, 1);
+}
+// Fills line.ends; the length of the line.
+__device__ __forceinline__ unsigned lay_out(const AttnParams &p, Line &line)
 {
     const int lane = lane_id(), wv = wave_id();
     const int per = (p.B + kAttnThreads - 1) / kAttnThreads, b0 = threadIdx.x * per;
-    int tiles[kMaxPerThread], blocks[kMaxPerThread];
-    float work = 0.0f;
+    unsigned sum[kMaxPerThread], total = 0;
 #pragma unroll
     for (int i = 0; i < kMaxPerThread; ++i) {
-        tiles[i] = blocks[i] = 0;
         if (i < per && b0 + i < p.B) {
             int first, n, seq;
             request_of(p, b0 + i, first, n, seq);
-            tiles[i] = (n * p.G + kRows - 1) / kRows;
-            blocks[i] = blocks_of(p, max(seq - n, 0), seq - 1).count;
-            work += (float)tiles[i] * (float)blocks[i];
+            const unsigned tiles = (unsigned)(n * p.G + kRows - 1) / kRows;
+            if (tiles > 0) total += tiles * blocks_per_tile(p, n, seq);
+            line.what[b0 + i] = (unsigned long long)first << 47 | (unsigned long long)n << 30 | (unsigned)seq;
         }
+        sum[i] = total;
     }
-    work = wave_sum(work);
-    if (threadIdx.x == 0) sh.found.b = -1;
-    if (lane == 0) sh.work[wv] = work;
+    unsigned before = (unsigned)wave_prefix_sum_i32((int)total);
+    if (lane == kWave - 1) line.sum[wv] = before;
+    before -= total;
     __syncthreads();
-    work = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) work += sh.work[w];
-    // (a little more than the quotient: the sum is rounded, and there are no more than p.parts + tiles workgroups)
-    const int chunk = max(kMinChunk, (int)(work * 1.0001f / (float)p.parts) + 1);
-    int nx = 0, nc = 0;
-#pragma unroll
-    for (int i = 0; i < kMaxPerThread; ++i) {
-        blocks[i] = max((blocks[i] + chunk - 1) / chunk, 1);      // parts of each of its tiles
-        nx += CUT ? (blocks[i] > 1 ? tiles[i] : 0) : tiles[i] * blocks[i];
-        nc += blocks[i] > 1 ? tiles[i] * blocks[i] : 0;
-    }
-    int sx = wave_prefix_sum_i32(nx), sc = wave_prefix_sum_i32(nc);
-    if (lane == kWave - 1) {
-        sh.sum[0][wv] = sx;
-        sh.sum[1][wv] = sc;
-    }
-    __syncthreads();
+    unsigned all = 0;
 #pragma unroll
     for (int w = 0; w < kAttnWaves; ++w) {
-        sx += w < wv ? sh.sum[0][w] : 0;
-        sc += w < wv ? sh.sum[1][w] : 0;
+        before += w < wv ? line.sum[w] : 0u;
+        all += line.sum[w];
     }
-    sx -= nx;
-    sc -= nc;
-    // the requests of this thread one by one: does x fall into one of them
 #pragma unroll
-    for (int i = 0; i < kMaxPerThread; ++i) {
-        const int items = CUT ? (blocks[i] > 1 ? tiles[i] : 0) : tiles[i] * blocks[i], at = x - sx;
-        if (at >= 0 && at < items) {
-            const int tile = CUT ? at : at / blocks[i];
-            sh.found.tile = tile;
-            sh.found.split = CUT ? 0 : at - tile * blocks[i];
-            sh.found.splits = blocks[i];
-            sh.found.item = sc + tile * blocks[i];
-            sh.found.b = b0 + i;
-        }
-        sx += items;
-        sc += blocks[i] > 1 ? tiles[i] * blocks[i] : 0;
-    }
+    for (int i = 0; i < kMaxPerThread; ++i)
+        if (i < per && b0 + i < p.B) line.ends[b0 + i] = before + sum[i];
     __syncthreads();
-    f = sh.found;
-    f.b = __builtin_amdgcn_readfirstlane(f.b);
-    f.tile = __builtin_amdgcn_readfirstlane(f.tile);
-    f.split = __builtin_amdgcn_readfirstlane(f.split);
-    f.splits = __builtin_amdgcn_readfirstlane(f.splits);
-    f.item = __builtin_amdgcn_readfirstlane(f.item);
-    return f.b >= 0;
+    return (unsigned)__builtin_amdgcn_readfirstlane((int)all);
+}
+__device__ __forceinline__ unsigned length_of(const AttnParams &p, unsigned total) { return max((unsigned)kMinLength, (total + p.parts - 1) / p.parts); }
+
+// The tile that block `at` of the line belongs to: its request, its number there, the line's blocks [begin, begin + count).
+struct Place {
+    int b, tile, first, n, seq;
+    unsigned begin, count;
+};
+__device__ __forceinline__ Place place_of(const AttnParams &p, const Line &line, unsigned at)
+{
+    int lo = 0, hi = p.B - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (line.ends[mid] > at) hi = mid;
+        else lo = mid + 1;
+    }
+    Place s;
+    s.b = __builtin_amdgcn_readfirstlane(lo);
+    const unsigned long long what = line.what[s.b];
+    const unsigned start = (unsigned)__builtin_amdgcn_readfirstlane(s.b > 0 ? (int)line.ends[s.b - 1] : 0);
+    const unsigned hi32 = (unsigned)__builtin_amdgcn_readfirstlane((int)(what >> 32)), lo32 = (unsigned)__builtin_amdgcn_readfirstlane((int)what);
+    s.first = (int)(hi32 >> 15);
+    s.n = (int)((hi32 & 0x7fffu) << 2 | lo32 >> 30);
+    s.seq = (int)(lo32 & 0x3fffffffu);
+    s.count = blocks_per_tile(p, s.n, s.seq);
+    s.tile = (int)((at - start) / s.count);
+    s.begin = start + (unsigned)s.tile * s.count;
+    return s;
 }
 
 // Join over the four lanes l, l ^ 16, l ^ 32, l ^ 48 that hold parts of one row.
@@ -168,6 +160,16 @@ __device__ __forceinline__ float row_sum(float v)
     v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
     const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// 16 bytes that this launch reads once: past the caches.  For loads that cover whole cache lines with one instruction, as those of the
+// values do (64 requests, 411 MB of bf16 cache: 79.6 -> 63.6 us); the keys' cover half lines, whose other half the hint would
+// have read again (a plain read of scattered pages: 5.9 TB/s without the hint either way, with it 6.8 for whole lines and 5.1 for
+// halves).
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 load_once(const void *at)
+{
+    return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(at)));
 }
 
 // 8 E4M3 codes as bf16 (exact).
@@ -187,40 +189,55 @@ struct RowState {
     f32x4 o[D / 16];
 };
 
-// One step of TN tokens from token t0 on (t0 a multiple of TN): scores, weights, second product.  pos: position of the lane's row
-// (-1: no row); pmin, pmax: least and greatest position of the tile's rows.
+// One step of TN tokens from token t0 on (t0 a multiple of TN), in three parts so that the next step's loads can be under way while
+// this one's products run: page numbers, keys and values, products.
 template <int D, bool F8>
 struct Step {
+    static constexpr int E = F8 ? 1 : 2;           // bytes of an element
     static constexpr int TN = F8 ? 64 : 32;        // tokens: 16 bytes of a channel from every lane
     static constexpr int NS = TN / 16;             // fragments of S^T
     static constexpr int LT = TN / 4;              // consecutive tokens of a lane
-    static constexpr int KL = D * (F8 ? 1 : 2) / 64;   // 16-byte loads of a key row by its four lanes
+    static constexpr int KL = D * E / 64;          // 16-byte loads of a key row by its four lanes
 
-    static __device__ __forceinline__ void run(const AttnParams &p, const int32_t *pages, int h, int t0, const bf16x8 (&q)[D / 32], int pos,
-                                               int pmin, int pmax, RowState<D> &s)
+    int kid, vid;                                  // page numbers of the lane's key rows and of its run of tokens
+    bool vok;
+    uint4 kw[NS][KL], vw[D / 16];
+
+    // This lane's token for the first fragment (the others follow 4 apart), and the first of its run.
+    static __device__ __forceinline__ int key_token(int t0) { return t0 + ((lane_id() & 15) >> 2) * LT + (lane_id() & 3); }
+    static __device__ __forceinline__ int run_token(int t0) { return t0 + (lane_id() >> 4) * LT; }
+
+    __device__ __forceinline__ void fetch_pages(const AttnParams &p, const int32_t *pages, int t0)
     {
-        const int lane = lane_id(), g = lane >> 4, c = lane & 15;
-        constexpr int E = F8 ? 1 : 2;
-        const uint8_t *kc = (const uint8_t *)p.k, *vc = (const uint8_t *)p.v;
-        // this lane's token for the first fragment, and its run of tokens
-        const int kt = t0 + (c >> 2) * LT + (c & 3), vt = t0 + g * LT;
-        const int kp = page_of(p, kt >> 4), vp = page_of(p, vt >> 4), last = p.max_pages - 1;
-        const int kid = pages[min(kp, last)], vid = pages[min(vp, last)];
-        const bool kok = kp <= last && (unsigned)kid < (unsigned)p.num_pages, vok = vp <= last && (unsigned)vid < (unsigned)p.num_pages;
+        const int last = p.max_pages - 1;
+        kid = pages[min(page_of(p, key_token(t0) >> 4), last)];
+        vid = pages[min(page_of(p, run_token(t0) >> 4), last)];
+    }
+
+    __device__ __forceinline__ void fetch(const AttnParams &p, int h, int t0)
+    {
+        const int kt = key_token(t0), vt = run_token(t0);
+        const int kp = page_of(p, kt >> 4), vp = page_of(p, vt >> 4);
+        const bool kok = kp < p.max_pages && (unsigned)kid < (unsigned)p.num_pages;
+        vok = vp < p.max_pages && (unsigned)vid < (unsigned)p.num_pages;
         const size_t head_bytes = (size_t)p.page_size * D * E;
         // (tokens without a page are read from the first page's start and not seen)
-        const uint8_t *ka = kc + ((size_t)(kok ? kid : 0) * p.KVH + h) * head_bytes + (kok ? kt - kp * p.page_size : 0) * (D * E) + g * 16;
-        const uint8_t *va = vc + ((size_t)(vok ? vid : 0) * p.KVH + h) * head_bytes +
-                            (size_t)(c * p.page_size + (vok ? vt - vp * p.page_size : 0)) * E;
-
-        uint4 kw[NS][KL], vw[D / 16];
+        const uint8_t *ka = (const uint8_t *)p.k + ((size_t)(kok ? kid : 0) * p.KVH + h) * head_bytes + (kok ? kt - kp * p.page_size : 0) * (D * E) +
+                            (lane_id() >> 4) * 16;
+        const uint8_t *va = (const uint8_t *)p.v + ((size_t)(vok ? vid : 0) * p.KVH + h) * head_bytes +
+                            (size_t)((lane_id() & 15) * p.page_size + (vok ? vt - vp * p.page_size : 0)) * E;
 #pragma unroll
         for (int j = 0; j < NS; ++j)
 #pragma unroll
             for (int i = 0; i < KL; ++i) kw[j][i] = *reinterpret_cast<const uint4 *>(ka + j * 4 * (D * E) + i * 64);
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t) vw[t] = *reinterpret_cast<const uint4 *>(va + (size_t)t * 16 * p.page_size * E);
+        for (int t = 0; t < D / 16; ++t) vw[t] = load_once(va + (size_t)t * 16 * p.page_size * E);
+    }
 
+    // Scores, weights, second product.  pos: position of the lane's row (-1: no row); pmin, pmax: least and greatest position of
+    // the tile's rows.
+    __device__ __forceinline__ void run(const AttnParams &p, int t0, const bf16x8 (&q)[D / 32], int pos, int pmin, int pmax, RowState<D> &s)
+    {
         f32x4 z[NS];
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
@@ -240,6 +257,7 @@ struct Step {
         for (int i = 0; i < LT; ++i) x[i] = z[i / 4][i % 4] * p.scale2;
         // Tokens that not every row of the tile sees.  A token that none sees may hold anything, also what is no number: its
         // value is replaced by zero, since zero times it would not be.
+        const int vt = run_token(t0);
         const bool in_window = p.window == 0 || t0 > pmax - p.window || t0 + TN <= p.sinks;
         if (!(t0 + TN - 1 <= pmin && in_window && __all(vok))) {
 #pragma unroll
@@ -333,104 +351,174 @@ __device__ __forceinline__ void write_out(const AttnParams &p, int t, int head, 
     if (p.lse && c0 == 0) p.lse[(size_t)t * (p.KVH * p.G) + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
-// One workgroup per (part of the context of a tile of 16 rows of a request, key head); the blocks of the part go round the four
-// waves, whose parts of the softmax are joined in LDS.
+// A length of the line of one key head per workgroup, a quarter of it per wave, in steps.  A wave goes through its quarter tile by tile.
+// A tile that lies in it whole is finished in its registers; of the first and the last, which in general do not, it leaves its part in
+// LDS, and when all waves are through, the parts of each tile are joined: to the finished rows, or to a part in the workspace if
+// the tile goes on in another workgroup.  (With all four waves on one tile after the other, each with its round trips for lengths,
+// queries and page numbers, 256 requests with an 8-bit cache took 137 us where this takes 118.)
 template <int D, bool F8>
-__global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnParams p)
+__global__ __launch_bounds__(kAttnThreads, 2) void attn_rows_kernel(AttnParams p)
 {
-    __shared__ FindShared sh;
-    __shared__ float sm[kAttnWaves][kRows], sl[kAttnWaves][kRows];
-    __shared__ __align__(16) float so[kAttnWaves][kRows][D + 4];
+    typedef Step<D, F8> S;
+    constexpr int kSteps = kBlock / S::TN;
+    constexpr int kRecords = 2 * kAttnWaves;
+    constexpr unsigned kNone = 0xffffffffu;
+    __shared__ Line line;
+    __shared__ unsigned rec[kRecords];              // begin of the tile that the part belongs to
+    __shared__ float sm[kRecords][kRows], sl[kRecords][kRows];
+    __shared__ __align__(16) float so[kRecords][kRows][D + 4];
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id()), h = blockIdx.y;
-    Found f;
-    if (!find_work<false>(p, blockIdx.x, sh, f)) return;
-    int first, n, seq;
-    request_of(p, f.b, first, n, seq);
-    const int r = f.tile * kRows + (lane & 15), rows = n * p.G;
-    const bool real = r < rows;
-    const int tok = real ? r / p.G : 0;
-    const int pos = real ? seq - n + tok : -1;
-    const int pmin = max(seq - n + f.tile * kRows / p.G, 0), pmax = seq - n + (min(f.tile * kRows + kRows, rows) - 1) / p.G;
-    bf16x8 q[D / 32];
-    load_queries<D, F8>(p.q + (size_t)(first + tok) * p.q_stride + (size_t)(h * p.G + (real ? r % p.G : 0)) * D, real, q);
+    const unsigned total = lay_out(p, line), length = length_of(p, total);
+    const unsigned from = min(blockIdx.x * length, total), to = min(from + length, total);
+    if (from >= to) return;
+    if (lane < 2) rec[2 * wv + lane] = kNone;
+    const unsigned quarter = (length * kSteps + kAttnWaves - 1) / kAttnWaves;
+    const unsigned wfrom = min(from * kSteps + wv * quarter, to * kSteps), wto = min(wfrom + quarter, to * kSteps);
+    for (unsigned at = wfrom; at < wto;) {
+        const Place f = place_of(p, line, at / kSteps);
+        const unsigned begin = f.begin * kSteps, i0 = at - begin, i1 = min(f.count * kSteps, wto - begin);
+        at = begin + i1;
 
-    RowState<D> s;
-    s.m = -INFINITY;
-    s.l = 0.0f;
+        const int r = f.tile * kRows + (lane & 15), rows = f.n * p.G;
+        const bool real = r < rows;
+        const int tok = real ? r / p.G : 0;
+        const int pos = real ? f.seq - f.n + tok : -1;
+        const int pmin = max(f.seq - f.n + f.tile * kRows / p.G, 0), pmax = f.seq - f.n + (min(f.tile * kRows + kRows, rows) - 1) / p.G;
+        bf16x8 q[D / 32];
+        load_queries<D, F8>(p.q + (size_t)(f.first + tok) * p.q_stride + (size_t)(h * p.G + (real ? r % p.G : 0)) * D, real, q);
+        RowState<D> s;
+        s.m = -INFINITY;
+        s.l = 0.0f;
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) s.o[t] = {0.0f, 0.0f, 0.0f, 0.0f};
-    const Blocks blocks = blocks_of(p, pmin, pmax);
-    const int per = (blocks.count + f.splits - 1) / f.splits, i0 = f.split * per, i1 = min(i0 + per, blocks.count);
-    const int32_t *row = p.table + (size_t)f.b * p.max_pages;
-    for (int i = i0 + wv; i < i1; i += kAttnWaves) {
-        const int blk = blocks.at(i);
-        const int32_t *pages = (blk + 1) * kBlock <= p.prefix_len ? p.prefix_table : row;
-        for (int t = 0; t < kBlock; t += Step<D, F8>::TN) Step<D, F8>::run(p, pages, h, blk * kBlock + t, q, pos, pmin, pmax, s);
-    }
-    s.l = row_sum(s.l);
-    if (lane < kRows) {
-        sm[wv][lane] = s.m;
-        sl[wv][lane] = s.l;
-    }
+        for (int t = 0; t < D / 16; ++t) s.o[t] = {0.0f, 0.0f, 0.0f, 0.0f};
+
+        // (tiles of one request lie on the line with as many blocks each: those past a tile's own are passed over)
+        const Blocks blocks = blocks_of(p, pmin, pmax);
+        const int j0 = (int)min(i0, (unsigned)(blocks.count * kSteps)), j1 = (int)min(i1, (unsigned)(blocks.count * kSteps));
+        const int32_t *row = p.table + (size_t)f.b * p.max_pages;
+        const auto token = [&](int j) { return blocks.at(j / kSteps) * kBlock + j % kSteps * S::TN; };
+        const auto pages = [&](int t0) { return t0 / kBlock * kBlock + kBlock <= p.prefix_len ? p.prefix_table : row; };
+        if (j0 < j1) {
+            S step[2];
+            int t0 = token(j0);
+            step[0].fetch_pages(p, pages(t0), t0);
+            step[0].fetch(p, h, t0);
+            int t1 = token(min(j0 + 1, j1 - 1));
+            step[1].fetch_pages(p, pages(t1), t1);
+            for (int j = j0; j < j1; j += 2) {
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) *reinterpret_cast<f32x4 *>(&so[wv][lane & 15][t * 16 + (lane >> 4) * 4]) = s.o[t];
+                for (int k = 0; k < 2; ++k) {
+                    if (j + k < j1) {
+                        // The page numbers of the step after the next, the next step's keys and values, this one's products.
+                        const int t2 = token(min(j + k + 2, j1 - 1));
+                        step[k].fetch_pages(p, pages(t2), t2);
+                        if (j + k + 1 < j1) step[k ^ 1].fetch(p, h, t1);
+                        step[k].run(p, t0, q, pos, pmin, pmax, s);
+                        t0 = t1;
+                        t1 = t2;
+                    }
+                }
+            }
+        }
+        s.l = row_sum(s.l);
+        if (i0 == 0 && i1 == f.count * kSteps) {
+            const float inv = s.l == 0.0f ? 0.0f : p.v_scale / s.l;
+            if (real) {
+                const int t = f.first + tok, head = h * p.G + r % p.G;
+                uint16_t *dst = p.out + (size_t)t * p.out_stride + (size_t)head * D + (lane >> 4) * 4;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+                    *reinterpret_cast<uint2 *>(dst + i * 16) = make_uint2(pack_bf16(s.o[i][0] * inv, s.o[i][1] * inv), pack_bf16(s.o[i][2] * inv, s.o[i][3] * inv));
+                if (p.lse && lane < 16) p.lse[(size_t)t * (p.KVH * p.G) + head] = s.l == 0.0f ? -INFINITY : (s.m + __log2f(s.l)) * kLn2;
+            }
+        } else {
+            const int k = 2 * wv + (at == wto && i0 == 0 ? 1 : 0);      // the wave's last tile, or its first
+            if (lane < kRows) {
+                sm[k][lane] = s.m;
+                sl[k][lane] = s.l;
+            }
+            if (lane == 0) rec[k] = f.begin;
+#pragma unroll
+            for (int t = 0; t < D / 16; ++t) *reinterpret_cast<f32x4 *>(&so[k][lane & 15][t * 16 + (lane >> 4) * 4]) = s.o[t];
+        }
+    }
     __syncthreads();
-    // 16 threads per row, D / 16 channels each
-    const int orow = threadIdx.x / kRows, c0 = threadIdx.x % kRows * (D / 16), ro = f.tile * kRows + orow;
-    if (ro >= rows) return;
-    float m = sm[0][orow];
+    // The parts in LDS, in the order of the line: those of one tile follow one another.  16 threads per row, D / 16 channels each.
+    const int recs = (int)rec[lane % kRecords];
+    const auto tile_of = [&](int k) { return (unsigned)__builtin_amdgcn_readlane(recs, k); };
+    const int orow = threadIdx.x / kRows, c0 = threadIdx.x % kRows * (D / 16);
+    for (int k = 0; k < kRecords;) {
+        const unsigned begin = tile_of(k);
+        int end = k + 1;
+        while (end < kRecords && (tile_of(end) == begin || tile_of(end) == kNone)) ++end;
+        if (begin == kNone) {
+            ++k;
+            continue;
+        }
+        const Place f = place_of(p, line, begin);
+        const int ro = f.tile * kRows + orow;
+        if (ro < f.n * p.G) {
+            float m = -INFINITY;
+            for (int w = k; w < end; ++w)
+                if (tile_of(w) == begin) m = fmaxf(m, sm[w][orow]);
+            float l = 0.0f, o[D / 16];
 #pragma unroll
-    for (int w = 1; w < kAttnWaves; ++w) m = fmaxf(m, sm[w][orow]);
-    float l = 0.0f, o[D / 16];
+            for (int i = 0; i < D / 16; ++i) o[i] = 0.0f;
+            for (int w = k; w < end; ++w) {
+                if (tile_of(w) != begin) continue;
+                const float e = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[w][orow] - m);
+                l += e * sl[w][orow];
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) o[i] = 0.0f;
+                for (int i = 0; i < D / 16; ++i) o[i] += e * so[w][orow][c0 + i];
+            }
+            if (begin >= from && begin + f.count <= to) {
+                write_out<D>(p, f.first + ro / p.G, h * p.G + ro % p.G, c0, m, l, o);
+            } else {
+                // (a workgroup cuts two tiles at most: the one it begins inside, and the one it ends in)
+                const size_t part = ((size_t)(2 * blockIdx.x + (begin >= from ? 1 : 0)) * p.KVH + h) * kRows + orow;
+                float4 *dst = reinterpret_cast<float4 *>(p.part_o + part * D + c0);
 #pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) {
-        const float e = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[w][orow] - m);
-        l += e * sl[w][orow];
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) o[i] += e * so[w][orow][c0 + i];
+                for (int i = 0; i < D / 64; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                if (c0 == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * part) = make_float2(m, l);
+            }
+        }
+        k = end;
     }
-    if (f.splits == 1) {
-        write_out<D>(p, first + ro / p.G, h * p.G + ro % p.G, c0, m, l, o);
-        return;
-    }
-    const size_t part = ((size_t)(f.item + f.split) * p.KVH + h) * kRows + orow;
-    float4 *dst = reinterpret_cast<float4 *>(p.part_o + part * D + c0);
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-    if (c0 == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * part) = make_float2(m, l);
 }
 
-// Joins the parts of a tile's rows.  Few rows with many parts each are the case that counts (one request alone: a few rows, dozens
-// of parts), so a tile's rows are spread over kJoinSlices workgroups, and the parts of a row over what is left of the
-// workgroup's D / 4-lane groups, which meet in LDS.
+// Joins the parts of the tiles that are cut.  Workgroup x has the x-th cut of the line; where it is the first that goes through a
+// tile, it joins the tile.  Few rows with many parts each are the case that counts (one request alone: a few rows, dozens of
+// parts), so a tile's rows are spread over kJoinSlices workgroups, and the parts of a row over what is left of the workgroup's
+// D / 4-lane groups, which meet in LDS.
 constexpr int kJoinSlices = 4;
 template <int D>
 __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p)
 {
     constexpr int L = D / 4, NG = kAttnThreads / L;         // lanes of a group (4 channels each), groups
-    __shared__ FindShared sh;
+    __shared__ Line line;
     __shared__ float sm[NG], sl[NG];
     __shared__ __align__(16) float4 so[NG][L];
-    Found f;
-    if (!find_work<true>(p, blockIdx.x, sh, f)) return;
-    int first, n, seq;
-    request_of(p, f.b, first, n, seq);
-    const int h = blockIdx.y, slice = blockIdx.z, here = min(n * p.G - f.tile * kRows, kRows);    // the tile's rows
+    const unsigned total = lay_out(p, line), length = length_of(p, total), cut = (blockIdx.x + 1) * length;
+    if (cut >= total) return;
+    const Place f = place_of(p, line, cut);
+    if (f.begin == cut || f.begin + length < cut) return;          // between two tiles, or not the first cut of this one
+    const int h = blockIdx.y, slice = blockIdx.z, here = min(f.n * p.G - f.tile * kRows, kRows);   // the tile's rows
     const int mine = (here - slice + kJoinSlices - 1) / kJoinSlices;                               // those of this workgroup
     if (mine <= 0) return;
     const int width = mine > 2 ? 4 : mine;                                                         // (a power of two)
     const int grp = threadIdx.x / L, lane = threadIdx.x % L, k = grp % width, sub = grp / width;
     const int orow = slice + k * kJoinSlices;
     const bool real = k < mine;
-    const size_t part = ((size_t)f.item * p.KVH + h) * kRows + (real ? orow : slice), step = (size_t)p.KVH * kRows;
+    const int parts = (int)((f.begin + f.count - 1) / length) - (int)blockIdx.x + 1;
     float m = -INFINITY, l = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-    for (int i = sub; i < f.splits; i += NG / width) {
-        const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * (part + i * step));
-        const f32x4 u = *reinterpret_cast<const f32x4 *>(p.part_o + (part + i * step) * D + 4 * lane);
+    for (int i = sub; i < parts; i += NG / width) {
+        // the first part is the last of its workgroup unless the tile begins where the workgroup does
+        const unsigned x = blockIdx.x + i;
+        const size_t part = ((size_t)(2 * x + (f.begin >= x * length ? 1 : 0)) * p.KVH + h) * kRows + (real ? orow : slice);
+        const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * part);
+        const f32x4 u = *reinterpret_cast<const f32x4 *>(p.part_o + part * D + 4 * lane);
         const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.0f : top;
         const float a = __builtin_amdgcn_exp2f(m - base), e = __builtin_amdgcn_exp2f(ml.x - base);
         l = l * a + e * ml.y;
@@ -452,23 +540,21 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p)
         o = o * a + f32x4{u.x, u.y, u.z, u.w} * e;
         m = top;
     }
-    const int ro = f.tile * kRows + orow, t = first + ro / p.G, head = h * p.G + ro % p.G;
+    const int ro = f.tile * kRows + orow, t = f.first + ro / p.G, head = h * p.G + ro % p.G;
     const float inv = l == 0.0f ? 0.0f : p.v_scale / l;
     *reinterpret_cast<uint2 *>(p.out + (size_t)t * p.out_stride + (size_t)head * D + 4 * lane) =
         make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
     if (p.lse && lane == 0) p.lse[(size_t)t * (p.KVH * p.G) + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
-// What the workspace holds: rows of unfinished parts, and their maxima and sums.  A tile that is cut has more than `chunk` blocks, so its
-// parts are fewer than twice blocks / chunk, and all such parts fewer than twice p.parts; there are at most p.parts such tiles.
+// What the workspace holds: rows of unfinished tiles with their maxima and sums, two tiles per workgroup.
 struct AttnSpace {
-    int tiles, parts;
+    int parts;
     size_t ml_off, total;
 };
-static AttnSpace attention_space(int B, int T, int QH, int KVH, int D)
+static AttnSpace attention_space(int KVH, int D)
 {
     AttnSpace w;
-    w.tiles = B + (int)((int64_t)T * (QH / KVH) / kRows);     // sum of ceil(rows / 16) over requests
     w.parts = kWorkgroups / KVH > 0 ? kWorkgroups / KVH : 1;
     const size_t rows = (size_t)2 * w.parts * KVH * kRows;
     w.ml_off = align256(rows * D * 4);
@@ -490,13 +576,17 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
         return fail(LYNX_ERR_UNSUPPORTED, "%s: need B<=%d, T<=%d, max_pages*page_size<=%d", who, LYNX_MAX_REQUESTS, LYNX_MAX_STEP_TOKENS, kMaxContext);
     if (prefix_len > max_pages * page_size)
         return fail(LYNX_ERR_INVALID_ARG, "%s: the prefix is longer than a row of the block table", who);
+    // (positions on the line of all tiles' blocks are 32 bits)
+    const int64_t most_tiles = B + (int64_t)T * (QH / KVH) / kRows;
+    if (most_tiles * (((int64_t)max_pages * page_size + kBlock - 1) / kBlock) >= (int64_t)1 << 31)
+        return fail(LYNX_ERR_UNSUPPORTED, "%s: need (B + T * QH / KVH / 16) * max_pages * page_size < 2^37", who);
     if (!(scale > 0.0f) || scale > 3.0e38f) return fail(LYNX_ERR_INVALID_ARG, "%s: scale must be finite and > 0", who);
     if (T == 0) return LYNX_OK;
     if (!block_table || !q_start || !seq_len || (prefix_len > 0 && !prefix_table) || !workspace)
         return fail(LYNX_ERR_INVALID_ARG, "%s: null pointer", who);
     if ((rc = check_rows(who, "q", q, q_stride, QH, D)) != LYNX_OK || (rc = check_rows(who, "out", out, out_stride, QH, D)) != LYNX_OK) return rc;
     if (((uintptr_t)workspace & 255) != 0) return fail(LYNX_ERR_INVALID_ARG, "%s: the workspace must start on 256 bytes", who);
-    const AttnSpace w = attention_space(B, T, QH, KVH, D);
+    const AttnSpace w = attention_space(KVH, D);
     AttnParams p = {q, k_cache, v_cache, block_table, q_start, seq_len, prefix_table, out, lse, q_stride, out_stride, B, T, KVH, QH / KVH,
                     num_pages, max_pages, page_size, prefix_len, page_multiplier(page_size), scale * k_scale * kLog2e, v_scale,
                     window < kMaxContext ? window : 0, sinks < kMaxContext ? sinks : kMaxContext,   // (a window that long hides nothing)
@@ -504,9 +594,9 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
     const bool f8 = cache_format == LYNX_CACHE_FP8;
     auto kernel = D == 128 ? (f8 ? attn_rows_kernel<128, true> : attn_rows_kernel<128, false>)
                            : (f8 ? attn_rows_kernel<64, true> : attn_rows_kernel<64, false>);
-    const bool cut = max_pages * page_size > kMinChunk * kBlock;       // else no context is long enough
-    hipLaunchKernelGGL(kernel, dim3(w.tiles + (cut ? w.parts : 0), KVH), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
-    if (cut) hipLaunchKernelGGL((D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>), dim3(w.tiles < w.parts ? w.tiles : w.parts, KVH, kJoinSlices), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
+    hipLaunchKernelGGL(kernel, dim3(w.parts, KVH), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
+    if (w.parts > 1)
+        hipLaunchKernelGGL((D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>), dim3(w.parts - 1, KVH, kJoinSlices), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
     return check_launch(who);
 }
 
@@ -515,7 +605,7 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
 extern "C" size_t lynx_attention_workspace_bytes(int B, int T, int QH, int KVH, int D, int prefix_len)
 {
     if (B <= 0 || T < 0 || QH <= 0 || KVH <= 0 || D <= 0 || prefix_len < 0) return 0;
-    return lynx::attention_space(B, T, QH, KVH, D).total;
+    return lynx::attention_space(KVH, D).total;
 }
 
 extern "C" int lynx_attention(const uint16_t *q, int64_t q_stride, const void *k_cache, const void *v_cache, int cache_format,
