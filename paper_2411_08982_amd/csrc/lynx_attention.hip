@@ -12,6 +12,9 @@
 //
 // Softmax in one pass: m = running maximum (of the scores times scale * log2 e), l = sum of 2^(s - m), O accumulates 2^(s - m) v; when
 // m grows, l and O are multiplied by 2^(m_old - m_new).  All in fp32.
+#include <algorithm>
+#include <climits>
+
 #include "lynx_attention.h"
 
 namespace lynx {
@@ -36,6 +39,9 @@ struct AttnParams {
     int window, sinks;
     int parts;                          // parts that the contexts of all tiles together are cut into, per key head
     float *part_o, *part_ml;            // workspace: unfinished rows
+    int narrow;                         // requests of more rows are left to attn_tiles_kernel
+    int wide_parts;                     // attn_tiles_kernel: parts that all its tiles' contexts are cut into, per key head
+    float *wide_o, *wide_ml;
 };
 
 // Page (index in a row of the table) of the 16 tokens from 16 * group on: group / (page_size / 16), by multiplication.
@@ -95,7 +101,7 @@ __device__ __forceinline__ unsigned lay_out(const AttnParams &p, Line &line)
         if (i < per && b0 + i < p.B) {
             int first, n, seq;
             request_of(p, b0 + i, first, n, seq);
-            const unsigned tiles = (unsigned)(n * p.G + kRows - 1) / kRows;
+            const unsigned tiles = n * p.G <= p.narrow ? (unsigned)(n * p.G + kRows - 1) / kRows : 0u;
             if (tiles > 0) total += tiles * blocks_per_tile(p, n, seq);
             line.what[b0 + i] = (unsigned long long)first << 47 | (unsigned long long)n << 30 | (unsigned)seq;
         }
@@ -547,18 +553,399 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p)
     if (p.lse && lane == 0) p.lse[(size_t)t * (p.KVH * p.G) + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
-// What the workspace holds: rows of unfinished tiles with their maxima and sums, two tiles per workgroup.
-struct AttnSpace {
-    int parts;
-    size_t ml_off, total;
+// ---- many rows ------------------------------------------------------------------------------------------------------------
+// Tiles of 128 rows, 32 to a wave, on v_mfma_f32_32x32x16_bf16: a block of 64 tokens is brought into LDS once for the four waves, in
+// two buffers, and every fragment that a wave reads there serves 32 rows.  The same transposed products as above: a lane has row
+// l % 32, and a result fragment of S^T gives it 16 tokens of a block's half; the keys lie in LDS in such an order that they are two
+// runs of 8 consecutive tokens, the operand of the second product.
+// What bounds it: per block and wave 32 matrix instructions (1024 cycles), 32 KiB from LDS (four waves: 1024 cycles of its 128 bytes
+// each) and about as many VALU cycles for 32 weights per lane; two workgroups a CU, so that one's softmax stands beside the
+// other's products.
+constexpr int kTileRows = 128;
+constexpr int kWaveRows = 32;
+constexpr int kMinChunk = 8;                // blocks: a part of a tile's context is not made shorter
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// The contexts of all tiles are cut into parts of at most `chunk` blocks, chunk following from the work of the whole batch, so that a
+// few tiles with long contexts fill the chip.  The parts of a request's last tile, the longest, come first.
+struct FindShared {
+    float work[kAttnWaves];
+    int sum[2][kAttnWaves];
+    int found[6];
 };
-static AttnSpace attention_space(int KVH, int D)
+struct Part {
+    int b, tile, split, splits, item;       // item: index of the tile's first part among those of all tiles that are cut
+};
+// CUT: x counts the tiles that are cut, otherwise the parts of all tiles.
+template <bool CUT>
+__device__ __forceinline__ bool find_part(const AttnParams &p, int x, FindShared &sh, Part &f)
+{
+    const int lane = lane_id(), wv = wave_id();
+    const int per = (p.B + kAttnThreads - 1) / kAttnThreads, b0 = threadIdx.x * per;
+    int tiles[kMaxPerThread], blocks[kMaxPerThread];
+    float work = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kMaxPerThread; ++i) {
+        tiles[i] = blocks[i] = 0;
+        if (i < per && b0 + i < p.B) {
+            int first, n, seq;
+            request_of(p, b0 + i, first, n, seq);
+            tiles[i] = n * p.G > p.narrow ? (n * p.G + kTileRows - 1) / kTileRows : 0;
+            blocks[i] = blocks_of(p, max(seq - n, 0), seq - 1).count;
+            work += (float)tiles[i] * (float)blocks[i];
+        }
+    }
+    work = wave_sum(work);
+    if (threadIdx.x == 0) sh.found[0] = -1;
+    if (lane == 0) sh.work[wv] = work;
+    __syncthreads();
+    work = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kAttnWaves; ++w) work += sh.work[w];
+    // (a little more than the quotient: the sum is rounded, and there are no more than p.wide_parts + tiles workgroups)
+    const int chunk = max(kMinChunk, (int)(work * 1.0001f / (float)p.wide_parts) + 1);
+    int nx = 0, nc = 0;
+#pragma unroll
+    for (int i = 0; i < kMaxPerThread; ++i) {
+        blocks[i] = max((blocks[i] + chunk - 1) / chunk, 1);      // parts of each of its tiles
+        nx += CUT ? (blocks[i] > 1 ? tiles[i] : 0) : tiles[i] * blocks[i];
+        nc += blocks[i] > 1 ? tiles[i] * blocks[i] : 0;
+    }
+    int sx = wave_prefix_sum_i32(nx), sc = wave_prefix_sum_i32(nc);
+    if (lane == kWave - 1) {
+        sh.sum[0][wv] = sx;
+        sh.sum[1][wv] = sc;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kAttnWaves; ++w) {
+        sx += w < wv ? sh.sum[0][w] : 0;
+        sc += w < wv ? sh.sum[1][w] : 0;
+    }
+    sx -= nx;
+    sc -= nc;
+#pragma unroll
+    for (int i = 0; i < kMaxPerThread; ++i) {
+        const int items = CUT ? (blocks[i] > 1 ? tiles[i] : 0) : tiles[i] * blocks[i], at = x - sx;
+        if (at >= 0 && at < items) {
+            const int k = CUT ? at : at / blocks[i];
+            sh.found[1] = tiles[i] - 1 - k;
+            sh.found[2] = CUT ? 0 : at - k * blocks[i];
+            sh.found[3] = blocks[i];
+            sh.found[4] = sc + k * blocks[i];
+            sh.found[0] = b0 + i;
+        }
+        sx += items;
+        sc += blocks[i] > 1 ? tiles[i] * blocks[i] : 0;
+    }
+    __syncthreads();
+    f.b = __builtin_amdgcn_readfirstlane(sh.found[0]);
+    f.tile = __builtin_amdgcn_readfirstlane(sh.found[1]);
+    f.split = __builtin_amdgcn_readfirstlane(sh.found[2]);
+    f.splits = __builtin_amdgcn_readfirstlane(sh.found[3]);
+    f.item = __builtin_amdgcn_readfirstlane(sh.found[4]);
+    return f.b >= 0;
+}
+
+__device__ __forceinline__ float half_max(float v)
+{
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float half_sum(float v)
+{
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// A block of 64 tokens on its way from the pages into LDS: 16 bytes per load and thread.
+//   keys [64][D]: row m holds token 16 (m / 16) + (m % 16 with bits 2 and 3 exchanged), see attn_tiles_kernel;
+//   values [D][64].  The 16-byte pieces of a row are stored at their place xor (row & 7): the lanes of a fragment read one column of
+//   pieces, which would all lie in the same banks.
+template <int D, bool F8>
+struct BlockLoad {
+    static constexpr int E = F8 ? 1 : 2;
+    static constexpr int KP = D * E / 16, VP = kBlock * E / 16;          // loads of a row
+    static constexpr int KI = kBlock * KP / kAttnThreads, VI = D * VP / kAttnThreads;
+    uint4 kw[KI], vw[VI];
+
+    // Lane l: number of the page of the block's l % 4th 16 tokens.
+    static __device__ __forceinline__ int fetch_pages(const AttnParams &p, const int32_t *pages, int blk)
+    {
+        const int idx = page_of(p, blk * (kBlock / 16) + (lane_id() & 3));
+        const int id = pages[min(idx, p.max_pages - 1)];
+        return idx < p.max_pages && (unsigned)id < (unsigned)p.num_pages ? id : -1;
+    }
+
+    __device__ __forceinline__ void fetch(const AttnParams &p, int h, int blk, int ids)
+    {
+        const int tid = threadIdx.x;
+        const size_t head_bytes = (size_t)p.page_size * D * E;
+#pragma unroll
+        for (int i = 0; i < KI; ++i) {
+            const int m = (i * kAttnThreads + tid) / KP, r = m & 15, tok = (r & 3) | (r & 4) << 1 | (r & 8) >> 1;
+            const int grp = m >> 4, at = blk * kBlock + grp * 16;
+            const int id = __shfl(ids, grp);
+            const int place = at - page_of(p, at >> 4) * p.page_size + tok;
+            const uint8_t *ka = (const uint8_t *)p.k + ((size_t)max(id, 0) * p.KVH + h) * head_bytes + (size_t)(id < 0 ? tok : place) * (D * E) +
+                                (tid % KP) * 16;
+            kw[i] = *reinterpret_cast<const uint4 *>(ka);
+        }
+        const int tok = tid % VP * (16 / E), at = blk * kBlock + (tok & ~15);
+        const int id = __shfl(ids, tok >> 4);
+        const int place = id < 0 ? tok & 15 : at - page_of(p, at >> 4) * p.page_size + (tok & 15);
+        const uint8_t *va = (const uint8_t *)p.v + ((size_t)max(id, 0) * p.KVH + h) * head_bytes + ((size_t)(tid / VP) * p.page_size + place) * E;
+#pragma unroll
+        for (int i = 0; i < VI; ++i) vw[i] = *reinterpret_cast<const uint4 *>(va + (size_t)i * (kAttnThreads / VP) * p.page_size * E);
+    }
+
+    // Values of tokens that no row of the tile sees become zero (they may be no numbers).
+    __device__ __forceinline__ void blank(const AttnParams &p, int blk, int ids, int pmin, int pmax)
+    {
+        const int tok = threadIdx.x % VP * (16 / E), t0 = blk * kBlock + tok;
+        const bool ok = __shfl(ids, tok >> 4) >= 0;
+        uint32_t mask[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            mask[w] = 0u;
+#pragma unroll
+            for (int i = 0; i < 4 / E; ++i) {
+                const int t = t0 + w * (4 / E) + i;
+                const bool any = ok && t <= pmax && (p.window == 0 || t > pmin - p.window || t < p.sinks);
+                mask[w] |= any ? (F8 ? 0xffu << (8 * i) : 0xffffu << (16 * i)) : 0u;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < VI; ++i) vw[i] = make_uint4(vw[i].x & mask[0], vw[i].y & mask[1], vw[i].z & mask[2], vw[i].w & mask[3]);
+    }
+
+    __device__ __forceinline__ void put(uint4 *kb, uint4 *vb) const
+    {
+        const int tid = threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < KI; ++i) {
+            const int m = (i * kAttnThreads + tid) / KP, c = tid % KP;
+            if (F8) {
+                kb[m * (D / 8) + ((2 * c) ^ (m & 7))] = __builtin_bit_cast(uint4, widen8(make_uint2(kw[i].x, kw[i].y)));
+                kb[m * (D / 8) + ((2 * c + 1) ^ (m & 7))] = __builtin_bit_cast(uint4, widen8(make_uint2(kw[i].z, kw[i].w)));
+            } else {
+                kb[m * (D / 8) + (c ^ (m & 7))] = kw[i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < VI; ++i) {
+            const int d = (i * kAttnThreads + tid) / VP, c = tid % VP;
+            if (F8) {
+                vb[d * 8 + ((2 * c) ^ (d & 7))] = __builtin_bit_cast(uint4, widen8(make_uint2(vw[i].x, vw[i].y)));
+                vb[d * 8 + ((2 * c + 1) ^ (d & 7))] = __builtin_bit_cast(uint4, widen8(make_uint2(vw[i].z, vw[i].w)));
+            } else {
+                vb[d * 8 + (c ^ (d & 7))] = vw[i];
+            }
+        }
+    }
+};
+
+template <int D, bool F8>
+__global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams p)
+{
+    typedef BlockLoad<D, F8> B;
+    __shared__ FindShared sh;
+    __shared__ __align__(16) uint4 kbuf[2][kBlock * D / 8], vbuf[2][kBlock * D / 8];
+    const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id()), h = blockIdx.y;
+    Part f;
+    if (!find_part<false>(p, blockIdx.x, sh, f)) return;
+    int first, n, seq;
+    request_of(p, f.b, first, n, seq);
+    const int rows = n * p.G, base = seq - n, r0 = f.tile * kTileRows + wv * kWaveRows, r = r0 + (lane & 31), hf = lane >> 5;
+    const bool real = r < rows;
+    const int tok = real ? r / p.G : 0, head = h * p.G + (real ? r % p.G : 0);
+    const int pos = real ? base + tok : -1;
+    const int tmin = max(base + f.tile * kTileRows / p.G, 0), tmax = base + (min(f.tile * kTileRows + kTileRows, rows) - 1) / p.G;
+    const int pmin = max(base + r0 / p.G, 0), pmax = r0 < rows ? base + (min(r0 + kWaveRows, rows) - 1) / p.G : -1;    // of the wave's rows
+    bf16x8 q[D / 16];
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+        uint4 u = make_uint4(0u, 0u, 0u, 0u);
+        if (real) u = *reinterpret_cast<const uint4 *>(p.q + (size_t)(first + tok) * p.q_stride + (size_t)head * D + i * 16 + hf * 8);
+        q[i] = __builtin_bit_cast(bf16x8, u);
+    }
+    float m = -INFINITY, l = 0.0f;
+    f32x16 o[D / 32];
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
+
+    const Blocks blocks = blocks_of(p, tmin, tmax);
+    const int per = (blocks.count + f.splits - 1) / f.splits, i0 = f.split * per, i1 = min(i0 + per, blocks.count);
+    const int32_t *pages = p.table + (size_t)f.b * p.max_pages;
+    B next;
+    int ids = 0, ids_next = 0;
+    if (i0 < i1) {
+        ids = B::fetch_pages(p, pages, blocks.at(i0));
+        ids_next = B::fetch_pages(p, pages, blocks.at(min(i0 + 1, i1 - 1)));
+        next.fetch(p, h, blocks.at(i0), ids);
+    }
+    for (int i = i0; i < i1; ++i) {
+        const int blk = blocks.at(i), t0 = blk * kBlock;
+        // the block's values and keys into LDS, the next one's on their way, this one's products
+        const bool all_ok = __all(ids >= 0);
+        if (t0 + kBlock - 1 > tmax || !all_ok || (p.window != 0 && t0 <= tmin - p.window && t0 + kBlock > p.sinks)) next.blank(p, blk, ids, tmin, tmax);
+        uint4 *kb = kbuf[(i - i0) & 1], *vb = vbuf[(i - i0) & 1];
+        next.put(kb, vb);
+        const int now = ids;
+        ids = ids_next;
+        if (i + 1 < i1) {
+            ids_next = B::fetch_pages(p, pages, blocks.at(min(i + 2, i1 - 1)));
+            next.fetch(p, h, blocks.at(i + 1), ids);
+        }
+        __syncthreads();
+        if (t0 > pmax || (p.window != 0 && t0 + kBlock - 1 <= pmin - p.window && t0 >= p.sinks)) continue;   // nothing for this wave
+
+        f32x16 z[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) z[t][j] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) {
+                const uint4 a = kb[(t * 32 + (lane & 31)) * (D / 8) + ((2 * j + hf) ^ (lane & 7))];
+                z[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), q[j], z[t], 0, 0, 0);
+            }
+        }
+        // lane: tokens t0 + 32 t + 16 (j / 8) + 8 hf + j % 8
+        const bool in_window = p.window == 0 || t0 > pmax - p.window || t0 + kBlock <= p.sinks;
+        if (!(t0 + kBlock - 1 <= pmin && in_window && all_ok)) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const bool ok = __builtin_amdgcn_readlane(now, 2 * t + s) >= 0;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int tt = t0 + 32 * t + 16 * s + 8 * hf + j;
+                        const bool seen = ok && tt <= pos && (p.window == 0 || tt > pos - p.window || tt < p.sinks);
+                        z[t][s * 8 + j] = seen ? z[t][s * 8 + j] : -INFINITY;
+                    }
+                }
+        }
+        float top = z[0][0];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, z[t][j]);
+        top = half_max(top) * p.scale2;
+        // m follows the maximum only when it is 8 behind: until then weights are up to 2^8, and rows are rescaled less often
+        if (__any(top > m + 8.0f)) {
+            const float up = fmaxf(m, top), a = up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - up);
+            l *= a;
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t) o[t] *= a;
+            m = up;
+        }
+        const float off = m == -INFINITY ? 0.0f : -m;
+        bf16x8 w[4];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                float e[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][s * 8 + j], p.scale2, off));
+                    l += e[j];
+                }
+                w[2 * t + s] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7])));
+            }
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const uint4 a = vb[(t * 32 + (lane & 31)) * 8 + ((2 * s + hf) ^ (lane & 7))];
+                o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), w[s], o[t], 0, 0, 0);
+            }
+    }
+    l = half_sum(l);
+    if (!real) return;
+    // lane: channels 32 t + 8 j + 4 hf .. + 3 of its row
+    if (f.splits == 1) {
+        const float inv = l == 0.0f ? 0.0f : p.v_scale / l;
+        uint16_t *dst = p.out + (size_t)(first + tok) * p.out_stride + (size_t)head * D + hf * 4;
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *reinterpret_cast<uint2 *>(dst + t * 32 + j * 8) = make_uint2(pack_bf16(o[t][4 * j] * inv, o[t][4 * j + 1] * inv),
+                                                                               pack_bf16(o[t][4 * j + 2] * inv, o[t][4 * j + 3] * inv));
+        if (p.lse && hf == 0) p.lse[(size_t)(first + tok) * (p.KVH * p.G) + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+    } else {
+        const size_t part = ((size_t)(f.item + f.split) * p.KVH + h) * kTileRows + (r - f.tile * kTileRows);
+        float *dst = p.wide_o + part * D + hf * 4;
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *reinterpret_cast<float4 *>(dst + t * 32 + j * 8) = make_float4(o[t][4 * j], o[t][4 * j + 1], o[t][4 * j + 2], o[t][4 * j + 3]);
+        if (hf == 0) *reinterpret_cast<float2 *>(p.wide_ml + 2 * part) = make_float2(m, l);
+    }
+}
+
+// Joins the parts of the tiles of attn_tiles_kernel that are cut: D / 4 lanes to a row.
+constexpr int kTileSlices = 8;
+template <int D>
+__global__ __launch_bounds__(kAttnThreads) void attn_join_tiles_kernel(AttnParams p)
+{
+    constexpr int L = D / 4, NG = kAttnThreads / L;
+    __shared__ FindShared sh;
+    Part f;
+    if (!find_part<true>(p, blockIdx.x, sh, f)) return;
+    int first, n, seq;
+    request_of(p, f.b, first, n, seq);
+    const int h = blockIdx.y, lane = threadIdx.x % L, here = min(n * p.G - f.tile * kTileRows, kTileRows);
+    for (int row = blockIdx.z * (kTileRows / kTileSlices) + threadIdx.x / L; row < min((int)(blockIdx.z + 1) * (kTileRows / kTileSlices), here); row += NG) {
+        const size_t part = ((size_t)f.item * p.KVH + h) * kTileRows + row, step = (size_t)p.KVH * kTileRows;
+        float m = -INFINITY, l = 0.0f;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int i = 0; i < f.splits; ++i) {
+            const float2 ml = *reinterpret_cast<const float2 *>(p.wide_ml + 2 * (part + i * step));
+            const f32x4 u = *reinterpret_cast<const f32x4 *>(p.wide_o + (part + i * step) * D + 4 * lane);
+            const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.0f : top;
+            const float a = __builtin_amdgcn_exp2f(m - base), e = __builtin_amdgcn_exp2f(ml.x - base);
+            l = l * a + e * ml.y;
+            o = o * a + u * e;
+            m = top;
+        }
+        const int ro = f.tile * kTileRows + row, t = first + ro / p.G, head = h * p.G + ro % p.G;
+        const float inv = l == 0.0f ? 0.0f : p.v_scale / l;
+        *reinterpret_cast<uint2 *>(p.out + (size_t)t * p.out_stride + (size_t)head * D + 4 * lane) =
+            make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+        if (p.lse && lane == 0) p.lse[(size_t)t * (p.KVH * p.G) + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+    }
+}
+
+// Requests of up to this many rows are read by tiles of 16 rows, others by tiles of 128.
+constexpr int kNarrowRows = 64;
+// What the workspace holds: rows of unfinished tiles with their maxima and sums.  attn_rows_kernel leaves two tiles per workgroup.
+// attn_tiles_kernel: a tile that is cut has more than `chunk` blocks, so its parts are fewer than twice blocks / chunk, all such
+// parts fewer than twice wide_parts, and such tiles at most wide_parts.
+struct AttnSpace {
+    int parts, wide_parts;
+    bool wide;
+    size_t ml_off, wide_o_off, wide_ml_off, total;
+};
+static AttnSpace attention_space(int T, int G, int KVH, int D)
 {
     AttnSpace w;
     w.parts = kWorkgroups / KVH > 0 ? kWorkgroups / KVH : 1;
     const size_t rows = (size_t)2 * w.parts * KVH * kRows;
     w.ml_off = align256(rows * D * 4);
-    w.total = w.ml_off + align256(rows * 8);
+    w.wide_o_off = w.ml_off + align256(rows * 8);
+    w.wide = (int64_t)T * G > kNarrowRows;
+    w.wide_parts = w.parts;
+    const size_t wide_rows = w.wide ? (size_t)2 * w.wide_parts * KVH * kTileRows : 0;
+    w.wide_ml_off = w.wide_o_off + align256(wide_rows * D * 4);
+    w.total = w.wide_ml_off + align256(wide_rows * 8);
     return w;
 }
 
@@ -586,14 +973,27 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
         return fail(LYNX_ERR_INVALID_ARG, "%s: null pointer", who);
     if ((rc = check_rows(who, "q", q, q_stride, QH, D)) != LYNX_OK || (rc = check_rows(who, "out", out, out_stride, QH, D)) != LYNX_OK) return rc;
     if (((uintptr_t)workspace & 255) != 0) return fail(LYNX_ERR_INVALID_ARG, "%s: the workspace must start on 256 bytes", who);
-    const AttnSpace w = attention_space(KVH, D);
+    const int G = QH / KVH;
+    const AttnSpace w = attention_space(T, G, KVH, D);
+    const bool wide = w.wide && (int64_t)max_new * G > kNarrowRows;
+    char *const ws = (char *)workspace;
     AttnParams p = {q, k_cache, v_cache, block_table, q_start, seq_len, prefix_table, out, lse, q_stride, out_stride, B, T, KVH, QH / KVH,
                     num_pages, max_pages, page_size, prefix_len, page_multiplier(page_size), scale * k_scale * kLog2e, v_scale,
                     window < kMaxContext ? window : 0, sinks < kMaxContext ? sinks : kMaxContext,   // (a window that long hides nothing)
-                    w.parts, (float *)workspace, (float *)((char *)workspace + w.ml_off)};
+                    w.parts, (float *)ws, (float *)(ws + w.ml_off), wide ? kNarrowRows : INT_MAX, w.wide_parts, (float *)(ws + w.wide_o_off),
+                    (float *)(ws + w.wide_ml_off)};
     const bool f8 = cache_format == LYNX_CACHE_FP8;
     auto kernel = D == 128 ? (f8 ? attn_rows_kernel<128, true> : attn_rows_kernel<128, false>)
                            : (f8 ? attn_rows_kernel<64, true> : attn_rows_kernel<64, false>);
+    if (wide) {
+        // tiles: sum of ceil(rows / 128) over requests of more than kNarrowRows rows
+        const int tiles = (int)((int64_t)T * G / kTileRows) + (int)std::min<int64_t>(B, (int64_t)T * G / kNarrowRows);
+        auto tiles_kernel = D == 128 ? (f8 ? attn_tiles_kernel<128, true> : attn_tiles_kernel<128, false>)
+                                     : (f8 ? attn_tiles_kernel<64, true> : attn_tiles_kernel<64, false>);
+        hipLaunchKernelGGL(tiles_kernel, dim3(tiles + w.wide_parts, KVH), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
+        hipLaunchKernelGGL((D == 128 ? attn_join_tiles_kernel<128> : attn_join_tiles_kernel<64>), dim3(std::min(tiles, w.wide_parts), KVH, kTileSlices),
+                           dim3(kAttnThreads), 0, (hipStream_t)stream, p);
+    }
     hipLaunchKernelGGL(kernel, dim3(w.parts, KVH), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
     if (w.parts > 1)
         hipLaunchKernelGGL((D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>), dim3(w.parts - 1, KVH, kJoinSlices), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
@@ -605,7 +1005,7 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
 extern "C" size_t lynx_attention_workspace_bytes(int B, int T, int QH, int KVH, int D, int prefix_len)
 {
     if (B <= 0 || T < 0 || QH <= 0 || KVH <= 0 || D <= 0 || prefix_len < 0) return 0;
-    return lynx::attention_space(KVH, D).total;
+    return lynx::attention_space(T, QH / KVH, KVH, D).total;
 }
 
 extern "C" int lynx_attention(const uint16_t *q, int64_t q_stride, const void *k_cache, const void *v_cache, int cache_format,
