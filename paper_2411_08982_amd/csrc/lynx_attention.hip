@@ -73,6 +73,12 @@ __device__ __forceinline__ Blocks blocks_of(const AttnParams &p, int pmin, int p
     return s;
 }
 
+// Whether some row at positions pmin .. pmax sees token t.  (Not by branches: the conditions are a few comparisons.)
+__device__ __forceinline__ int seen(const AttnParams &p, int t, int pmin, int pmax)
+{
+    return (int)(t <= pmax) & ((int)(p.window == 0) | (int)(t > pmin - p.window) | (int)(t < p.sinks));
+}
+
 // How the work is cut.  The blocks of all tiles, one tile after the other, are one long line that is cut into equal lengths, one
 // for each workgroup that the chip holds at once: however ragged the contexts, all workgroups read the same amount (with whole tiles
 // dealt out, 64 requests of 500 to 12000 tokens took 100 us where the equal cut takes 71).  A tile that a cut goes through is
@@ -267,19 +273,14 @@ struct Step {
         const bool in_window = p.window == 0 || t0 > pmax - p.window || t0 + TN <= p.sinks;
         if (!(t0 + TN - 1 <= pmin && in_window && __all(vok))) {
 #pragma unroll
-            for (int i = 0; i < LT; ++i) {
-                const int t = vt + i;
-                const bool seen = vok && t <= pos && (p.window == 0 || t > pos - p.window || t < p.sinks);
-                x[i] = seen ? x[i] : -INFINITY;
-            }
+            for (int i = 0; i < LT; ++i) x[i] = (int)vok & seen(p, vt + i, pos, pos) ? x[i] : -INFINITY;
             uint32_t mask[4];
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 mask[w] = 0u;
 #pragma unroll
                 for (int i = 0; i < 4 / E; ++i) {
-                    const int t = vt + w * (4 / E) + i;
-                    const bool any = vok && t <= pmax && (p.window == 0 || t > pmin - p.window || t < p.sinks);
+                    const int any = (int)vok & seen(p, vt + w * (4 / E) + i, pmin, pmax);
                     mask[w] |= any ? (F8 ? 0xffu << (8 * i) : 0xffffu << (16 * i)) : 0u;
                 }
             }
@@ -658,18 +659,33 @@ __device__ __forceinline__ float half_sum(float v)
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// A block of 64 tokens on its way from the pages into LDS: 16 bytes per load and thread.
+// A block of 64 tokens on its way from the pages into LDS: 16 bytes per load and thread.  Each of the block's four groups of 16 tokens
+// lies in one page; what one load instruction brings is of one group, so that its address is a scalar and a constant of the lane.
 //   keys [64][D]: row m holds token 16 (m / 16) + (m % 16 with bits 2 and 3 exchanged), see attn_tiles_kernel;
-//   values [D][64].  The 16-byte pieces of a row are stored at their place xor (row & 7): the lanes of a fragment read one column of
-//   pieces, which would all lie in the same banks.
+//   values [D][64]; wave w brings group w.  The 16-byte pieces of a row are stored at their place xor (row & 7): the lanes of a
+//   fragment read one column of pieces, which would all lie in the same banks.
 template <int D, bool F8>
 struct BlockLoad {
     static constexpr int E = F8 ? 1 : 2;
-    static constexpr int KP = D * E / 16, VP = kBlock * E / 16;          // loads of a row
-    static constexpr int KI = kBlock * KP / kAttnThreads, VI = D * VP / kAttnThreads;
-    uint4 kw[KI], vw[VI];
+    static constexpr int KP = D * E / 16;                                // loads of a key row
+    static constexpr int KI = kBlock * KP / kAttnThreads;
+    static constexpr int VP = E;                                         // loads of a group of one channel
+    static constexpr int VI = D * VP / kWave;
+    u32x4 kw[KI], vw[VI];
+    unsigned koff, voff;          // the lane's places in a group of keys and of values (bytes), and in LDS (16-byte pieces)
+    int kput, vput;
 
-    // Lane l: number of the page of the block's l % 4th 16 tokens.
+    __device__ __forceinline__ BlockLoad(const AttnParams &p)
+    {
+        const int tid = threadIdx.x, lane = lane_id(), wv = wave_id();
+        const int m = tid / KP, r = m & 15, tok = (r & 3) | (r & 4) << 1 | (r & 8) >> 1, d = lane / VP;
+        koff = (unsigned)(tok * (D * E) + tid % KP * 16);
+        voff = (unsigned)(d * p.page_size + lane % VP * 8) * E;
+        kput = m * (D / 8) + ((tid % KP * (2 / E)) ^ (m & 7));
+        vput = d * 8 + ((2 * wv + (F8 ? 0 : lane % VP)) ^ (d & 7));
+    }
+
+    // Lane l: number of the page of the block's l % 4th 16 tokens, -1 if there is none.
     static __device__ __forceinline__ int fetch_pages(const AttnParams &p, const int32_t *pages, int blk)
     {
         const int idx = page_of(p, blk * (kBlock / 16) + (lane_id() & 3));
@@ -677,69 +693,61 @@ struct BlockLoad {
         return idx < p.max_pages && (unsigned)id < (unsigned)p.num_pages ? id : -1;
     }
 
-    __device__ __forceinline__ void fetch(const AttnParams &p, int h, int blk, int ids)
+    __device__ __forceinline__ void fetch(const AttnParams &p, int h, int wv, int blk, int ids)
     {
-        const int tid = threadIdx.x;
         const size_t head_bytes = (size_t)p.page_size * D * E;
+        const auto group = [&](int g, const void *cache, int token_bytes) {
+            const int id = __builtin_amdgcn_readlane(ids, g), at = blk * (kBlock / 16) + g;
+            const int place = id < 0 ? 0 : at * 16 - page_of(p, at) * p.page_size;
+            return (const uint8_t *)cache + ((size_t)max(id, 0) * p.KVH + h) * head_bytes + (size_t)(place * token_bytes);
+        };
 #pragma unroll
-        for (int i = 0; i < KI; ++i) {
-            const int m = (i * kAttnThreads + tid) / KP, r = m & 15, tok = (r & 3) | (r & 4) << 1 | (r & 8) >> 1;
-            const int grp = m >> 4, at = blk * kBlock + grp * 16;
-            const int id = __shfl(ids, grp);
-            const int place = at - page_of(p, at >> 4) * p.page_size + tok;
-            const uint8_t *ka = (const uint8_t *)p.k + ((size_t)max(id, 0) * p.KVH + h) * head_bytes + (size_t)(id < 0 ? tok : place) * (D * E) +
-                                (tid % KP) * 16;
-            kw[i] = *reinterpret_cast<const uint4 *>(ka);
-        }
-        const int tok = tid % VP * (16 / E), at = blk * kBlock + (tok & ~15);
-        const int id = __shfl(ids, tok >> 4);
-        const int place = id < 0 ? tok & 15 : at - page_of(p, at >> 4) * p.page_size + (tok & 15);
-        const uint8_t *va = (const uint8_t *)p.v + ((size_t)max(id, 0) * p.KVH + h) * head_bytes + ((size_t)(tid / VP) * p.page_size + place) * E;
+        for (int i = 0; i < KI; ++i)
+            kw[i] = *reinterpret_cast<const u32x4 *>(group((i * kAttnThreads + wv * kWave) / (16 * KP), p.k, D * E) + koff);
+        const uint8_t *va = group(wv, p.v, E);
 #pragma unroll
-        for (int i = 0; i < VI; ++i) vw[i] = *reinterpret_cast<const uint4 *>(va + (size_t)i * (kAttnThreads / VP) * p.page_size * E);
+        for (int i = 0; i < VI; ++i) vw[i] = *reinterpret_cast<const u32x4 *>(va + (size_t)i * (kWave / VP) * p.page_size * E + voff);
     }
 
     // Values of tokens that no row of the tile sees become zero (they may be no numbers).
-    __device__ __forceinline__ void blank(const AttnParams &p, int blk, int ids, int pmin, int pmax)
+    __device__ __forceinline__ void blank(const AttnParams &p, int wv, int blk, int ids, int pmin, int pmax)
     {
-        const int tok = threadIdx.x % VP * (16 / E), t0 = blk * kBlock + tok;
-        const bool ok = __shfl(ids, tok >> 4) >= 0;
-        uint32_t mask[4];
+        const int t0 = blk * kBlock + 16 * wv + (F8 ? 0 : (int)(lane_id() % VP) * 8);
+        const bool ok = __builtin_amdgcn_readlane(ids, wv) >= 0;
+        u32x4 mask;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             mask[w] = 0u;
 #pragma unroll
             for (int i = 0; i < 4 / E; ++i) {
-                const int t = t0 + w * (4 / E) + i;
-                const bool any = ok && t <= pmax && (p.window == 0 || t > pmin - p.window || t < p.sinks);
+                const int any = (int)ok & seen(p, t0 + w * (4 / E) + i, pmin, pmax);
                 mask[w] |= any ? (F8 ? 0xffu << (8 * i) : 0xffffu << (16 * i)) : 0u;
             }
         }
 #pragma unroll
-        for (int i = 0; i < VI; ++i) vw[i] = make_uint4(vw[i].x & mask[0], vw[i].y & mask[1], vw[i].z & mask[2], vw[i].w & mask[3]);
+        for (int i = 0; i < VI; ++i) vw[i] &= mask;
     }
 
-    __device__ __forceinline__ void put(uint4 *kb, uint4 *vb) const
+    __device__ __forceinline__ void put(u32x4 *kb, u32x4 *vb) const
     {
-        const int tid = threadIdx.x;
 #pragma unroll
         for (int i = 0; i < KI; ++i) {
-            const int m = (i * kAttnThreads + tid) / KP, c = tid % KP;
+            u32x4 *dst = kb + kput + i * (kAttnThreads / KP) * (D / 8);
             if (F8) {
-                kb[m * (D / 8) + ((2 * c) ^ (m & 7))] = __builtin_bit_cast(uint4, widen8(make_uint2(kw[i].x, kw[i].y)));
-                kb[m * (D / 8) + ((2 * c + 1) ^ (m & 7))] = __builtin_bit_cast(uint4, widen8(make_uint2(kw[i].z, kw[i].w)));
+                dst[0] = __builtin_bit_cast(u32x4, widen8(make_uint2(kw[i].x, kw[i].y)));
+                kb[(kput ^ 1) + i * (kAttnThreads / KP) * (D / 8)] = __builtin_bit_cast(u32x4, widen8(make_uint2(kw[i].z, kw[i].w)));
             } else {
-                kb[m * (D / 8) + (c ^ (m & 7))] = kw[i];
+                dst[0] = kw[i];
             }
         }
 #pragma unroll
         for (int i = 0; i < VI; ++i) {
-            const int d = (i * kAttnThreads + tid) / VP, c = tid % VP;
+            u32x4 *dst = vb + vput + i * (kWave / VP) * 8;
             if (F8) {
-                vb[d * 8 + ((2 * c) ^ (d & 7))] = __builtin_bit_cast(uint4, widen8(make_uint2(vw[i].x, vw[i].y)));
-                vb[d * 8 + ((2 * c + 1) ^ (d & 7))] = __builtin_bit_cast(uint4, widen8(make_uint2(vw[i].z, vw[i].w)));
+                dst[0] = __builtin_bit_cast(u32x4, widen8(make_uint2(vw[i].x, vw[i].y)));
+                vb[(vput ^ 1) + i * (kWave / VP) * 8] = __builtin_bit_cast(u32x4, widen8(make_uint2(vw[i].z, vw[i].w)));
             } else {
-                vb[d * 8 + (c ^ (d & 7))] = vw[i];
+                dst[0] = vw[i];
             }
         }
     }
@@ -750,7 +758,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
 {
     typedef BlockLoad<D, F8> B;
     __shared__ FindShared sh;
-    __shared__ __align__(16) uint4 kbuf[2][kBlock * D / 8], vbuf[2][kBlock * D / 8];
+    __shared__ __align__(16) u32x4 kbuf[2][kBlock * D / 8], vbuf[2][kBlock * D / 8];
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id()), h = blockIdx.y;
     Part f;
     if (!find_part<false>(p, blockIdx.x, sh, f)) return;
@@ -765,8 +773,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
     bf16x8 q[D / 16];
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
-        uint4 u = make_uint4(0u, 0u, 0u, 0u);
-        if (real) u = *reinterpret_cast<const uint4 *>(p.q + (size_t)(first + tok) * p.q_stride + (size_t)head * D + i * 16 + hf * 8);
+        u32x4 u = {0u, 0u, 0u, 0u};
+        if (real) u = *reinterpret_cast<const u32x4 *>(p.q + (size_t)(first + tok) * p.q_stride + (size_t)head * D + i * 16 + hf * 8);
         q[i] = __builtin_bit_cast(bf16x8, u);
     }
     float m = -INFINITY, l = 0.0f;
@@ -779,25 +787,25 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
     const Blocks blocks = blocks_of(p, tmin, tmax);
     const int per = (blocks.count + f.splits - 1) / f.splits, i0 = f.split * per, i1 = min(i0 + per, blocks.count);
     const int32_t *pages = p.table + (size_t)f.b * p.max_pages;
-    B next;
+    B next(p);
     int ids = 0, ids_next = 0;
     if (i0 < i1) {
         ids = B::fetch_pages(p, pages, blocks.at(i0));
         ids_next = B::fetch_pages(p, pages, blocks.at(min(i0 + 1, i1 - 1)));
-        next.fetch(p, h, blocks.at(i0), ids);
+        next.fetch(p, h, wv, blocks.at(i0), ids);
     }
     for (int i = i0; i < i1; ++i) {
         const int blk = blocks.at(i), t0 = blk * kBlock;
         // the block's values and keys into LDS, the next one's on their way, this one's products
         const bool all_ok = __all(ids >= 0);
-        if (t0 + kBlock - 1 > tmax || !all_ok || (p.window != 0 && t0 <= tmin - p.window && t0 + kBlock > p.sinks)) next.blank(p, blk, ids, tmin, tmax);
-        uint4 *kb = kbuf[(i - i0) & 1], *vb = vbuf[(i - i0) & 1];
+        if (t0 + kBlock - 1 > tmax || !all_ok || (p.window != 0 && t0 <= tmin - p.window && t0 + kBlock > p.sinks)) next.blank(p, wv, blk, ids, tmin, tmax);
+        u32x4 *kb = kbuf[(i - i0) & 1], *vb = vbuf[(i - i0) & 1];
         next.put(kb, vb);
         const int now = ids;
         ids = ids_next;
         if (i + 1 < i1) {
             ids_next = B::fetch_pages(p, pages, blocks.at(min(i + 2, i1 - 1)));
-            next.fetch(p, h, blocks.at(i + 1), ids);
+            next.fetch(p, h, wv, blocks.at(i + 1), ids);
         }
         __syncthreads();
         if (t0 > pmax || (p.window != 0 && t0 + kBlock - 1 <= pmin - p.window && t0 >= p.sinks)) continue;   // nothing for this wave
@@ -809,7 +817,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
             for (int j = 0; j < 16; ++j) z[t][j] = 0.0f;
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) {
-                const uint4 a = kb[(t * 32 + (lane & 31)) * (D / 8) + ((2 * j + hf) ^ (lane & 7))];
+                const u32x4 a = kb[(t * 32 + (lane & 31)) * (D / 8) + ((2 * j + hf) ^ (lane & 7))];
                 z[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), q[j], z[t], 0, 0, 0);
             }
         }
@@ -823,9 +831,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
                     const bool ok = __builtin_amdgcn_readlane(now, 2 * t + s) >= 0;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const int tt = t0 + 32 * t + 16 * s + 8 * hf + j;
-                        const bool seen = ok && tt <= pos && (p.window == 0 || tt > pos - p.window || tt < p.sinks);
-                        z[t][s * 8 + j] = seen ? z[t][s * 8 + j] : -INFINITY;
+                        const int at = t0 + 32 * t + 16 * s + 8 * hf + j;
+                        z[t][s * 8 + j] = (int)ok & seen(p, at, pos, pos) ? z[t][s * 8 + j] : -INFINITY;
                     }
                 }
         }
@@ -861,7 +868,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
         for (int t = 0; t < D / 32; ++t)
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                const uint4 a = vb[(t * 32 + (lane & 31)) * 8 + ((2 * s + hf) ^ (lane & 7))];
+                const u32x4 a = vb[(t * 32 + (lane & 31)) * 8 + ((2 * s + hf) ^ (lane & 7))];
                 o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), w[s], o[t], 0, 0, 0);
             }
     }
