@@ -21,6 +21,7 @@ namespace lynx {
 
 constexpr int kBlock = 64;              // tokens of a block: the unit in which a row's context is dealt out
 constexpr int kRows = 16;               // rows of a tile
+constexpr int kTileRows = 128;          // rows of a tile of the kernel for many rows
 constexpr int kAttnThreads = 256;
 constexpr int kAttnWaves = kAttnThreads / kWave;
 constexpr int kWorkgroups = 512;       // workgroups that the chip holds at once: two of four waves on each of 256 CUs
@@ -33,7 +34,7 @@ struct AttnParams {
     uint16_t *out;
     float *lse;
     int64_t q_stride, out_stride;
-    int B, T, KVH, G, num_pages, max_pages, page_size, prefix_len;
+    int B, T, KVH, G, num_pages, max_pages, page_size;
     unsigned page_mul;                  // division of a group of 16 tokens by the page size: page_of
     float scale2, v_scale;              // scale * k_scale * log2 e
     int window, sinks;
@@ -42,6 +43,9 @@ struct AttnParams {
     int narrow;                         // requests of more rows are left to attn_tiles_kernel
     int wide_parts;                     // attn_tiles_kernel: parts that all its tiles' contexts are cut into, per key head
     float *wide_o, *wide_ml;
+    int prefix_blocks, prefix_splits;   // whole blocks of the shared prefix, and the parts that they are cut into
+    float *prefix_o, *prefix_ml;        // the parts of all rows,
+    float *own_o, *own_ml;              // and what the rows behind the prefix see of their own sequences
 };
 
 // Page (index in a row of the table) of the 16 tokens from 16 * group on: group / (page_size / 16), by multiplication.
@@ -57,17 +61,22 @@ __device__ __forceinline__ void request_of(const AttnParams &p, int b, int &firs
     seq = min(max(p.seq_len[b], 0), p.max_pages * p.page_size);
 }
 
-// The blocks that a span of rows at positions pmin .. pmax sees: `lead` blocks of the first tokens that stay visible, then those from
-// `start` on; `count` in all.
+// Whether the new tokens of a request, from position `base` on, all lie behind the whole blocks of the shared prefix: then those blocks
+// are left to the prefix's tiles.
+__device__ __forceinline__ bool behind_prefix(const AttnParams &p, int base) { return p.prefix_blocks > 0 && base >= p.prefix_blocks * kBlock; }
+
+// The blocks that a span of rows at positions pmin .. pmax of a request sees: `lead` blocks of the first tokens that stay visible, then
+// those from `start` on; `count` in all.
 struct Blocks {
     int lead, start, count;
     __device__ __forceinline__ int at(int i) const { return i < lead ? i : start + i - lead; }
 };
-__device__ __forceinline__ Blocks blocks_of(const AttnParams &p, int pmin, int pmax)
+__device__ __forceinline__ Blocks blocks_of(const AttnParams &p, int base, int pmin, int pmax)
 {
     Blocks s;
     const int end = pmax >= 0 ? pmax / kBlock + 1 : 0;
     s.start = p.window == 0 ? 0 : min(max(pmin - p.window + 1, 0) / kBlock, end);
+    if (behind_prefix(p, base)) s.start = p.prefix_blocks;
     s.lead = p.window == 0 ? 0 : min((p.sinks - 1 + kBlock) / kBlock, s.start);
     s.count = s.lead + end - s.start;
     return s;
@@ -94,7 +103,7 @@ struct Line {
 // Blocks of each tile of a request: those that its last rows and its first see together, so no tile has more; one at least.
 __device__ __forceinline__ unsigned blocks_per_tile(const AttnParams &p, int n, int seq)
 {
-    return (unsigned)max(blocks_of(p, max(seq - n, 0), seq - 1).count, 1);
+    return (unsigned)max(blocks_of(p, seq - n, max(seq - n, 0), seq - 1).count, 1);
 }
 // Fills line.ends; the length of the line.
 __device__ __forceinline__ unsigned lay_out(const AttnParams &p, Line &line)
@@ -343,19 +352,24 @@ __device__ __forceinline__ void load_queries(const uint16_t *row, bool real, bf1
     }
 }
 
-// A finished row piece of D / 16 channels: out = o * v_scale / l.
-template <int D>
-__device__ __forceinline__ void write_out(const AttnParams &p, int t, int head, int c0, float m, float l, const float (&o)[D / 16])
+// Finishes a row of which this lane has N runs of four channels, c0, c0 + step, ..: divides and writes.  A row that lies behind the
+// prefix is left in the workspace instead, for attn_finish_kernel.
+template <int D, int N>
+__device__ __forceinline__ void finish_row(const AttnParams &p, int t, int head, bool behind, int c0, int step, float m, float l, const f32x4 (&o)[N])
 {
+    const size_t row = (size_t)t * (p.KVH * p.G) + head;
+    if (behind) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) *reinterpret_cast<f32x4 *>(p.own_o + row * D + c0 + k * step) = o[k];
+        if (c0 == 0) *reinterpret_cast<float2 *>(p.own_ml + 2 * row) = make_float2(m, l);
+        return;
+    }
     const float inv = l == 0.0f ? 0.0f : p.v_scale / l;
     uint16_t *dst = p.out + (size_t)t * p.out_stride + (size_t)head * D + c0;
-    if (D == 128) {
-        *reinterpret_cast<uint4 *>(dst) = make_uint4(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv),
-                                                     pack_bf16(o[D / 16 - 4] * inv, o[D / 16 - 3] * inv), pack_bf16(o[D / 16 - 2] * inv, o[D / 16 - 1] * inv));
-    } else {
-        *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
-    }
-    if (p.lse && c0 == 0) p.lse[(size_t)t * (p.KVH * p.G) + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        *reinterpret_cast<uint2 *>(dst + k * step) = make_uint2(pack_bf16(o[k][0] * inv, o[k][1] * inv), pack_bf16(o[k][2] * inv, o[k][3] * inv));
+    if (p.lse && c0 == 0) p.lse[row] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
 // A length of the line of one key head per workgroup, a quarter of it per wave, in steps.  A wave goes through its quarter tile by tile.
@@ -400,25 +414,24 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_rows_kernel(AttnParams p
         for (int t = 0; t < D / 16; ++t) s.o[t] = {0.0f, 0.0f, 0.0f, 0.0f};
 
         // (tiles of one request lie on the line with as many blocks each: those past a tile's own are passed over)
-        const Blocks blocks = blocks_of(p, pmin, pmax);
+        const Blocks blocks = blocks_of(p, f.seq - f.n, pmin, pmax);
         const int j0 = (int)min(i0, (unsigned)(blocks.count * kSteps)), j1 = (int)min(i1, (unsigned)(blocks.count * kSteps));
         const int32_t *row = p.table + (size_t)f.b * p.max_pages;
         const auto token = [&](int j) { return blocks.at(j / kSteps) * kBlock + j % kSteps * S::TN; };
-        const auto pages = [&](int t0) { return t0 / kBlock * kBlock + kBlock <= p.prefix_len ? p.prefix_table : row; };
         if (j0 < j1) {
             S step[2];
             int t0 = token(j0);
-            step[0].fetch_pages(p, pages(t0), t0);
+            step[0].fetch_pages(p, row, t0);
             step[0].fetch(p, h, t0);
             int t1 = token(min(j0 + 1, j1 - 1));
-            step[1].fetch_pages(p, pages(t1), t1);
+            step[1].fetch_pages(p, row, t1);
             for (int j = j0; j < j1; j += 2) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     if (j + k < j1) {
                         // The page numbers of the step after the next, the next step's keys and values, this one's products.
                         const int t2 = token(min(j + k + 2, j1 - 1));
-                        step[k].fetch_pages(p, pages(t2), t2);
+                        step[k].fetch_pages(p, row, t2);
                         if (j + k + 1 < j1) step[k ^ 1].fetch(p, h, t1);
                         step[k].run(p, t0, q, pos, pmin, pmax, s);
                         t0 = t1;
@@ -429,15 +442,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_rows_kernel(AttnParams p
         }
         s.l = row_sum(s.l);
         if (i0 == 0 && i1 == f.count * kSteps) {
-            const float inv = s.l == 0.0f ? 0.0f : p.v_scale / s.l;
-            if (real) {
-                const int t = f.first + tok, head = h * p.G + r % p.G;
-                uint16_t *dst = p.out + (size_t)t * p.out_stride + (size_t)head * D + (lane >> 4) * 4;
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i)
-                    *reinterpret_cast<uint2 *>(dst + i * 16) = make_uint2(pack_bf16(s.o[i][0] * inv, s.o[i][1] * inv), pack_bf16(s.o[i][2] * inv, s.o[i][3] * inv));
-                if (p.lse && lane < 16) p.lse[(size_t)t * (p.KVH * p.G) + head] = s.l == 0.0f ? -INFINITY : (s.m + __log2f(s.l)) * kLn2;
-            }
+            if (real) finish_row<D>(p, f.first + tok, h * p.G + r % p.G, behind_prefix(p, f.seq - f.n), (lane >> 4) * 4, 16, s.m, s.l, s.o);
         } else {
             const int k = 2 * wv + (at == wto && i0 == 0 ? 1 : 0);      // the wave's last tile, or its first
             if (lane < kRows) {
@@ -468,24 +473,24 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_rows_kernel(AttnParams p
             float m = -INFINITY;
             for (int w = k; w < end; ++w)
                 if (tile_of(w) == begin) m = fmaxf(m, sm[w][orow]);
-            float l = 0.0f, o[D / 16];
+            float l = 0.0f;
+            f32x4 o[D / 64];
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i) o[i] = 0.0f;
+            for (int i = 0; i < D / 64; ++i) o[i] = {0.0f, 0.0f, 0.0f, 0.0f};
             for (int w = k; w < end; ++w) {
                 if (tile_of(w) != begin) continue;
                 const float e = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[w][orow] - m);
                 l += e * sl[w][orow];
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) o[i] += e * so[w][orow][c0 + i];
+                for (int i = 0; i < D / 64; ++i) o[i] += *reinterpret_cast<const f32x4 *>(&so[w][orow][c0 + 4 * i]) * e;
             }
             if (begin >= from && begin + f.count <= to) {
-                write_out<D>(p, f.first + ro / p.G, h * p.G + ro % p.G, c0, m, l, o);
+                finish_row<D>(p, f.first + ro / p.G, h * p.G + ro % p.G, behind_prefix(p, f.seq - f.n), c0, 4, m, l, o);
             } else {
                 // (a workgroup cuts two tiles at most: the one it begins inside, and the one it ends in)
                 const size_t part = ((size_t)(2 * blockIdx.x + (begin >= from ? 1 : 0)) * p.KVH + h) * kRows + orow;
-                float4 *dst = reinterpret_cast<float4 *>(p.part_o + part * D + c0);
 #pragma unroll
-                for (int i = 0; i < D / 64; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                for (int i = 0; i < D / 64; ++i) *reinterpret_cast<f32x4 *>(p.part_o + part * D + c0 + 4 * i) = o[i];
                 if (c0 == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * part) = make_float2(m, l);
             }
         }
@@ -547,11 +552,9 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p)
         o = o * a + f32x4{u.x, u.y, u.z, u.w} * e;
         m = top;
     }
-    const int ro = f.tile * kRows + orow, t = f.first + ro / p.G, head = h * p.G + ro % p.G;
-    const float inv = l == 0.0f ? 0.0f : p.v_scale / l;
-    *reinterpret_cast<uint2 *>(p.out + (size_t)t * p.out_stride + (size_t)head * D + 4 * lane) =
-        make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
-    if (p.lse && lane == 0) p.lse[(size_t)t * (p.KVH * p.G) + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+    const int ro = f.tile * kRows + orow;
+    f32x4 own[1] = {o};
+    finish_row<D>(p, f.first + ro / p.G, h * p.G + ro % p.G, behind_prefix(p, f.seq - f.n), 4 * lane, 4, m, l, own);
 }
 
 // ---- many rows ------------------------------------------------------------------------------------------------------------
@@ -562,7 +565,6 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p)
 // What bounds it: per block and wave 32 matrix instructions (1024 cycles), 32 KiB from LDS (four waves: 1024 cycles of its 128 bytes
 // each) and about as many VALU cycles for 32 weights per lane; two workgroups a CU, so that one's softmax stands beside the
 // other's products.
-constexpr int kTileRows = 128;
 constexpr int kWaveRows = 32;
 constexpr int kMinChunk = 8;                // blocks: a part of a tile's context is not made shorter
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -592,7 +594,7 @@ __device__ __forceinline__ bool find_part(const AttnParams &p, int x, FindShared
             int first, n, seq;
             request_of(p, b0 + i, first, n, seq);
             tiles[i] = n * p.G > p.narrow ? (n * p.G + kTileRows - 1) / kTileRows : 0;
-            blocks[i] = blocks_of(p, max(seq - n, 0), seq - 1).count;
+            blocks[i] = blocks_of(p, seq - n, max(seq - n, 0), seq - 1).count;
             work += (float)tiles[i] * (float)blocks[i];
         }
     }
@@ -753,17 +755,27 @@ struct BlockLoad {
     }
 };
 
-template <int D, bool F8>
+// PREFIX: the rows are those of the whole batch, whatever request they belong to, and the context is the shared prefix's whole blocks,
+// which all of them see; every row's part is left in the workspace.
+template <int D, bool F8, bool PREFIX>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams p)
 {
     typedef BlockLoad<D, F8> B;
     __shared__ FindShared sh;
     __shared__ __align__(16) u32x4 kbuf[2][kBlock * D / 8], vbuf[2][kBlock * D / 8];
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id()), h = blockIdx.y;
+    constexpr int kFar = 1 << 30;                   // behind every token of a prefix
     Part f;
-    if (!find_part<false>(p, blockIdx.x, sh, f)) return;
     int first, n, seq;
-    request_of(p, f.b, first, n, seq);
+    if (PREFIX) {
+        f = {0, (int)blockIdx.x / p.prefix_splits, (int)blockIdx.x % p.prefix_splits, p.prefix_splits, 0};
+        first = 0;
+        n = p.T;
+        seq = kFar + p.T;
+    } else {
+        if (!find_part<false>(p, blockIdx.x, sh, f)) return;
+        request_of(p, f.b, first, n, seq);
+    }
     const int rows = n * p.G, base = seq - n, r0 = f.tile * kTileRows + wv * kWaveRows, r = r0 + (lane & 31), hf = lane >> 5;
     const bool real = r < rows;
     const int tok = real ? r / p.G : 0, head = h * p.G + (real ? r % p.G : 0);
@@ -784,9 +796,9 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
 
-    const Blocks blocks = blocks_of(p, tmin, tmax);
+    const Blocks blocks = PREFIX ? Blocks{0, 0, p.prefix_blocks} : blocks_of(p, base, tmin, tmax);
     const int per = (blocks.count + f.splits - 1) / f.splits, i0 = f.split * per, i1 = min(i0 + per, blocks.count);
-    const int32_t *pages = p.table + (size_t)f.b * p.max_pages;
+    const int32_t *pages = PREFIX ? p.prefix_table : p.table + (size_t)f.b * p.max_pages;
     B next(p);
     int ids = 0, ids_next = 0;
     if (i0 < i1) {
@@ -875,25 +887,19 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
     l = half_sum(l);
     if (!real) return;
     // lane: channels 32 t + 8 j + 4 hf .. + 3 of its row
-    if (f.splits == 1) {
-        const float inv = l == 0.0f ? 0.0f : p.v_scale / l;
-        uint16_t *dst = p.out + (size_t)(first + tok) * p.out_stride + (size_t)head * D + hf * 4;
+    f32x4 c[D / 8];
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t)
+    for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                *reinterpret_cast<uint2 *>(dst + t * 32 + j * 8) = make_uint2(pack_bf16(o[t][4 * j] * inv, o[t][4 * j + 1] * inv),
-                                                                               pack_bf16(o[t][4 * j + 2] * inv, o[t][4 * j + 3] * inv));
-        if (p.lse && hf == 0) p.lse[(size_t)(first + tok) * (p.KVH * p.G) + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+        for (int j = 0; j < 4; ++j) c[4 * t + j] = {o[t][4 * j], o[t][4 * j + 1], o[t][4 * j + 2], o[t][4 * j + 3]};
+    if (!PREFIX && f.splits == 1) {
+        finish_row<D>(p, first + tok, head, behind_prefix(p, base), hf * 4, 8, m, l, c);
     } else {
-        const size_t part = ((size_t)(f.item + f.split) * p.KVH + h) * kTileRows + (r - f.tile * kTileRows);
-        float *dst = p.wide_o + part * D + hf * 4;
+        const size_t part = ((size_t)(PREFIX ? f.tile * f.splits + f.split : f.item + f.split) * p.KVH + h) * kTileRows + (r - f.tile * kTileRows);
+        float *dst = (PREFIX ? p.prefix_o : p.wide_o) + part * D + hf * 4;
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                *reinterpret_cast<float4 *>(dst + t * 32 + j * 8) = make_float4(o[t][4 * j], o[t][4 * j + 1], o[t][4 * j + 2], o[t][4 * j + 3]);
-        if (hf == 0) *reinterpret_cast<float2 *>(p.wide_ml + 2 * part) = make_float2(m, l);
+        for (int k = 0; k < D / 8; ++k) *reinterpret_cast<f32x4 *>(dst + k * 8) = c[k];
+        if (hf == 0) *reinterpret_cast<float2 *>((PREFIX ? p.prefix_ml : p.wide_ml) + 2 * part) = make_float2(m, l);
     }
 }
 
@@ -923,12 +929,47 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_tiles_kernel(AttnParam
             o = o * a + u * e;
             m = top;
         }
-        const int ro = f.tile * kTileRows + row, t = first + ro / p.G, head = h * p.G + ro % p.G;
-        const float inv = l == 0.0f ? 0.0f : p.v_scale / l;
-        *reinterpret_cast<uint2 *>(p.out + (size_t)t * p.out_stride + (size_t)head * D + 4 * lane) =
-            make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
-        if (p.lse && lane == 0) p.lse[(size_t)t * (p.KVH * p.G) + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+        const int ro = f.tile * kTileRows + row;
+        f32x4 own[1] = {o};
+        finish_row<D>(p, first + ro / p.G, h * p.G + ro % p.G, behind_prefix(p, seq - n), 4 * lane, 4, m, l, own);
     }
+}
+
+// Rows behind the shared prefix: joins the prefix's parts and the row's own.  D / 4 lanes to a row, rows in the order of out.
+template <int D>
+__global__ __launch_bounds__(kAttnThreads) void attn_finish_kernel(AttnParams p)
+{
+    constexpr int L = D / 4, NG = kAttnThreads / L;
+    __shared__ int starts[LYNX_MAX_REQUESTS];
+    for (int b = threadIdx.x; b < p.B; b += kAttnThreads) starts[b] = p.q_start[b];
+    const int QH = p.KVH * p.G, row = blockIdx.x * NG + threadIdx.x / L, lane = threadIdx.x % L;
+    const int t = row / QH, head = row % QH, h = head / p.G, r = t * p.G + head % p.G;
+    __syncthreads();
+    if (t >= p.T) return;
+    // the last request that begins at t or before
+    int lo = 0, hi = p.B - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (starts[mid] <= t) lo = mid;
+        else hi = mid - 1;
+    }
+    int first, n, seq;
+    request_of(p, lo, first, n, seq);
+    if (t < first || t >= first + n || !behind_prefix(p, seq - n)) return;
+    float m = p.own_ml[2 * (size_t)row], l = p.own_ml[2 * (size_t)row + 1];
+    f32x4 o[1] = {*reinterpret_cast<const f32x4 *>(p.own_o + (size_t)row * D + 4 * lane)};
+    size_t part = ((size_t)(r / kTileRows) * p.prefix_splits * p.KVH + h) * kTileRows + r % kTileRows;
+#pragma unroll 8
+    for (int i = 0; i < p.prefix_splits; ++i, part += (size_t)p.KVH * kTileRows) {
+        const float2 ml = *reinterpret_cast<const float2 *>(p.prefix_ml + 2 * part);
+        const f32x4 u = *reinterpret_cast<const f32x4 *>(p.prefix_o + part * D + 4 * lane);
+        const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.0f : top;
+        const float a = __builtin_amdgcn_exp2f(m - base), e = __builtin_amdgcn_exp2f(ml.x - base);
+        l = l * a + e * ml.y;
+        o[0] = o[0] * a + u * e;
+        m = top;
+    }
+    finish_row<D>(p, t, head, false, 4 * lane, 4, m, l, o);
 }
 
 // Requests of up to this many rows are read by tiles of 16 rows, others by tiles of 128.
@@ -936,12 +977,13 @@ constexpr int kNarrowRows = 64;
 // What the workspace holds: rows of unfinished tiles with their maxima and sums.  attn_rows_kernel leaves two tiles per workgroup.
 // attn_tiles_kernel: a tile that is cut has more than `chunk` blocks, so its parts are fewer than twice blocks / chunk, all such
 // parts fewer than twice wide_parts, and such tiles at most wide_parts.
+// The prefix's tiles leave every row's parts, and the rows behind the prefix their own.
 struct AttnSpace {
-    int parts, wide_parts;
+    int parts, wide_parts, prefix_tiles, prefix_splits;
     bool wide;
-    size_t ml_off, wide_o_off, wide_ml_off, total;
+    size_t ml_off, wide_o_off, wide_ml_off, prefix_o_off, prefix_ml_off, own_o_off, own_ml_off, total;
 };
-static AttnSpace attention_space(int T, int G, int KVH, int D)
+static AttnSpace attention_space(int T, int G, int KVH, int D, int prefix_len)
 {
     AttnSpace w;
     w.parts = kWorkgroups / KVH > 0 ? kWorkgroups / KVH : 1;
@@ -952,7 +994,17 @@ static AttnSpace attention_space(int T, int G, int KVH, int D)
     w.wide_parts = w.parts;
     const size_t wide_rows = w.wide ? (size_t)2 * w.wide_parts * KVH * kTileRows : 0;
     w.wide_ml_off = w.wide_o_off + align256(wide_rows * D * 4);
-    w.total = w.wide_ml_off + align256(wide_rows * 8);
+    w.prefix_o_off = w.wide_ml_off + align256(wide_rows * 8);
+    // as many parts of the prefix as fill the chip, of four blocks at least
+    const int blocks = prefix_len / kBlock;
+    w.prefix_tiles = (int)(((int64_t)T * G + kTileRows - 1) / kTileRows);
+    w.prefix_splits = blocks > 0 && T > 0 ? std::max(1, std::min(kWorkgroups / (w.prefix_tiles * KVH), (blocks + 3) / 4)) : 0;
+    const size_t prefix_rows = (size_t)w.prefix_tiles * w.prefix_splits * KVH * kTileRows;
+    w.prefix_ml_off = w.prefix_o_off + align256(prefix_rows * D * 4);
+    w.own_o_off = w.prefix_ml_off + align256(prefix_rows * 8);
+    const size_t own_rows = w.prefix_splits > 0 ? (size_t)T * G * KVH : 0;
+    w.own_ml_off = w.own_o_off + align256(own_rows * D * 4);
+    w.total = w.own_ml_off + align256(own_rows * 8);
     return w;
 }
 
@@ -981,22 +1033,28 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
     if ((rc = check_rows(who, "q", q, q_stride, QH, D)) != LYNX_OK || (rc = check_rows(who, "out", out, out_stride, QH, D)) != LYNX_OK) return rc;
     if (((uintptr_t)workspace & 255) != 0) return fail(LYNX_ERR_INVALID_ARG, "%s: the workspace must start on 256 bytes", who);
     const int G = QH / KVH;
-    const AttnSpace w = attention_space(T, G, KVH, D);
+    const AttnSpace w = attention_space(T, G, KVH, D, prefix_len);
     const bool wide = w.wide && (int64_t)max_new * G > kNarrowRows;
     char *const ws = (char *)workspace;
     AttnParams p = {q, k_cache, v_cache, block_table, q_start, seq_len, prefix_table, out, lse, q_stride, out_stride, B, T, KVH, QH / KVH,
-                    num_pages, max_pages, page_size, prefix_len, page_multiplier(page_size), scale * k_scale * kLog2e, v_scale,
+                    num_pages, max_pages, page_size, page_multiplier(page_size), scale * k_scale * kLog2e, v_scale,
                     window < kMaxContext ? window : 0, sinks < kMaxContext ? sinks : kMaxContext,   // (a window that long hides nothing)
                     w.parts, (float *)ws, (float *)(ws + w.ml_off), wide ? kNarrowRows : INT_MAX, w.wide_parts, (float *)(ws + w.wide_o_off),
-                    (float *)(ws + w.wide_ml_off)};
+                    (float *)(ws + w.wide_ml_off), prefix_len / kBlock, w.prefix_splits, (float *)(ws + w.prefix_o_off), (float *)(ws + w.prefix_ml_off),
+                    (float *)(ws + w.own_o_off), (float *)(ws + w.own_ml_off)};
     const bool f8 = cache_format == LYNX_CACHE_FP8;
     auto kernel = D == 128 ? (f8 ? attn_rows_kernel<128, true> : attn_rows_kernel<128, false>)
                            : (f8 ? attn_rows_kernel<64, true> : attn_rows_kernel<64, false>);
+    if (p.prefix_blocks > 0) {
+        auto prefix_kernel = D == 128 ? (f8 ? attn_tiles_kernel<128, true, true> : attn_tiles_kernel<128, false, true>)
+                                      : (f8 ? attn_tiles_kernel<64, true, true> : attn_tiles_kernel<64, false, true>);
+        hipLaunchKernelGGL(prefix_kernel, dim3(w.prefix_tiles * w.prefix_splits, KVH), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
+    }
     if (wide) {
         // tiles: sum of ceil(rows / 128) over requests of more than kNarrowRows rows
         const int tiles = (int)((int64_t)T * G / kTileRows) + (int)std::min<int64_t>(B, (int64_t)T * G / kNarrowRows);
-        auto tiles_kernel = D == 128 ? (f8 ? attn_tiles_kernel<128, true> : attn_tiles_kernel<128, false>)
-                                     : (f8 ? attn_tiles_kernel<64, true> : attn_tiles_kernel<64, false>);
+        auto tiles_kernel = D == 128 ? (f8 ? attn_tiles_kernel<128, true, false> : attn_tiles_kernel<128, false, false>)
+                                     : (f8 ? attn_tiles_kernel<64, true, false> : attn_tiles_kernel<64, false, false>);
         hipLaunchKernelGGL(tiles_kernel, dim3(tiles + w.wide_parts, KVH), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
         hipLaunchKernelGGL((D == 128 ? attn_join_tiles_kernel<128> : attn_join_tiles_kernel<64>), dim3(std::min(tiles, w.wide_parts), KVH, kTileSlices),
                            dim3(kAttnThreads), 0, (hipStream_t)stream, p);
@@ -1004,6 +1062,9 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
     hipLaunchKernelGGL(kernel, dim3(w.parts, KVH), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
     if (w.parts > 1)
         hipLaunchKernelGGL((D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>), dim3(w.parts - 1, KVH, kJoinSlices), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
+    if (p.prefix_blocks > 0)
+        hipLaunchKernelGGL((D == 128 ? attn_finish_kernel<128> : attn_finish_kernel<64>), dim3((unsigned)(((int64_t)T * QH * (D / 4) + kAttnThreads - 1) / kAttnThreads)),
+                           dim3(kAttnThreads), 0, (hipStream_t)stream, p);
     return check_launch(who);
 }
 
@@ -1012,7 +1073,7 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
 extern "C" size_t lynx_attention_workspace_bytes(int B, int T, int QH, int KVH, int D, int prefix_len)
 {
     if (B <= 0 || T < 0 || QH <= 0 || KVH <= 0 || D <= 0 || prefix_len < 0) return 0;
-    return lynx::attention_space(T, QH / KVH, KVH, D).total;
+    return lynx::attention_space(T, QH / KVH, KVH, D, prefix_len).total;
 }
 
 extern "C" int lynx_attention(const uint16_t *q, int64_t q_stride, const void *k_cache, const void *v_cache, int cache_format,
