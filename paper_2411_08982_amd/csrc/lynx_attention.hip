@@ -36,6 +36,7 @@ struct AttnParams {
     int64_t q_stride, out_stride;
     int B, T, KVH, G, num_pages, max_pages, page_size;
     unsigned page_mul;                  // division of a group of 16 tokens by the page size: page_of
+    unsigned group_mul, parts_mul;      // division of rows by G (token_of) and of the line by parts (length_of)
     float scale2, v_scale;              // scale * k_scale * log2 e
     int window, sinks;
     int parts;                          // parts that the contexts of all tiles together are cut into, per key head
@@ -51,6 +52,9 @@ struct AttnParams {
 // Page (index in a row of the table) of the 16 tokens from 16 * group on: group / (page_size / 16), by multiplication.
 // Exact for group < 2^25 and page_size / 16 <= 64, since group * error < 2^31 / (page_size / 16).
 __device__ __forceinline__ int page_of(const AttnParams &p, int group) { return (int)__umulhi(2u * (unsigned)group, p.page_mul); }
+// Token of row r: r / G, by multiplication.  Exact: r < 2^24 and G <= 256, so r * error < 2^32.
+__device__ __forceinline__ int token_of(const AttnParams &p, int r) { return p.G == 1 ? r : (int)__umulhi((unsigned)r, p.group_mul); }
+inline unsigned reciprocal(int d) { return d > 1 ? (unsigned)(((uint64_t)1 << 32) / (unsigned)d) + 1u : 0u; }
 inline unsigned page_multiplier(int page_size) { return (1u << 31) / (unsigned)(page_size / 16) + 1u; }
 
 // The rows of request b and its length, clamped.
@@ -138,7 +142,7 @@ __device__ __forceinline__ unsigned lay_out(const AttnParams &p, Line &line)
     __syncthreads();
     return (unsigned)__builtin_amdgcn_readfirstlane((int)all);
 }
-__device__ __forceinline__ unsigned length_of(const AttnParams &p, unsigned total) { return max((unsigned)kMinLength, (total + p.parts - 1) / p.parts); }
+__device__ __forceinline__ unsigned length_of(const AttnParams &p, unsigned total) { return max((unsigned)kMinLength, (p.parts == 1 ? total : __umulhi(total, p.parts_mul)) + 1u); }
 
 // The tile that block `at` of the line belongs to: its request, its number there, the line's blocks [begin, begin + count).
 struct Place {
@@ -162,7 +166,7 @@ __device__ __forceinline__ Place place_of(const AttnParams &p, const Line &line,
     s.n = (int)((hi32 & 0x7fffu) << 2 | lo32 >> 30);
     s.seq = (int)(lo32 & 0x3fffffffu);
     s.count = blocks_per_tile(p, s.n, s.seq);
-    s.tile = (int)((at - start) / s.count);
+    s.tile = s.n * p.G <= kRows ? 0 : (int)((at - start) / s.count);
     s.begin = start + (unsigned)s.tile * s.count;
     return s;
 }
@@ -402,11 +406,11 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_rows_kernel(AttnParams p
 
         const int r = f.tile * kRows + (lane & 15), rows = f.n * p.G;
         const bool real = r < rows;
-        const int tok = real ? r / p.G : 0;
+        const int tok = real ? token_of(p, r) : 0, head = h * p.G + (real ? r - tok * p.G : 0);
         const int pos = real ? f.seq - f.n + tok : -1;
-        const int pmin = max(f.seq - f.n + f.tile * kRows / p.G, 0), pmax = f.seq - f.n + (min(f.tile * kRows + kRows, rows) - 1) / p.G;
+        const int pmin = max(f.seq - f.n + token_of(p, f.tile * kRows), 0), pmax = f.seq - f.n + token_of(p, min(f.tile * kRows + kRows, rows) - 1);
         bf16x8 q[D / 32];
-        load_queries<D, F8>(p.q + (size_t)(f.first + tok) * p.q_stride + (size_t)(h * p.G + (real ? r % p.G : 0)) * D, real, q);
+        load_queries<D, F8>(p.q + (size_t)(f.first + tok) * p.q_stride + (size_t)head * D, real, q);
         RowState<D> s;
         s.m = -INFINITY;
         s.l = 0.0f;
@@ -442,7 +446,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_rows_kernel(AttnParams p
         }
         s.l = row_sum(s.l);
         if (i0 == 0 && i1 == f.count * kSteps) {
-            if (real) finish_row<D>(p, f.first + tok, h * p.G + r % p.G, behind_prefix(p, f.seq - f.n), (lane >> 4) * 4, 16, s.m, s.l, s.o);
+            if (real) finish_row<D>(p, f.first + tok, head, behind_prefix(p, f.seq - f.n), (lane >> 4) * 4, 16, s.m, s.l, s.o);
         } else {
             const int k = 2 * wv + (at == wto && i0 == 0 ? 1 : 0);      // the wave's last tile, or its first
             if (lane < kRows) {
@@ -485,7 +489,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_rows_kernel(AttnParams p
                 for (int i = 0; i < D / 64; ++i) o[i] += *reinterpret_cast<const f32x4 *>(&so[w][orow][c0 + 4 * i]) * e;
             }
             if (begin >= from && begin + f.count <= to) {
-                finish_row<D>(p, f.first + ro / p.G, h * p.G + ro % p.G, behind_prefix(p, f.seq - f.n), c0, 4, m, l, o);
+                const int tok = token_of(p, ro);
+                finish_row<D>(p, f.first + tok, h * p.G + ro - tok * p.G, behind_prefix(p, f.seq - f.n), c0, 4, m, l, o);
             } else {
                 // (a workgroup cuts two tiles at most: the one it begins inside, and the one it ends in)
                 const size_t part = ((size_t)(2 * blockIdx.x + (begin >= from ? 1 : 0)) * p.KVH + h) * kRows + orow;
@@ -552,9 +557,9 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p)
         o = o * a + f32x4{u.x, u.y, u.z, u.w} * e;
         m = top;
     }
-    const int ro = f.tile * kRows + orow;
+    const int ro = f.tile * kRows + orow, tok = token_of(p, ro);
     f32x4 own[1] = {o};
-    finish_row<D>(p, f.first + ro / p.G, h * p.G + ro % p.G, behind_prefix(p, f.seq - f.n), 4 * lane, 4, m, l, own);
+    finish_row<D>(p, f.first + tok, h * p.G + ro - tok * p.G, behind_prefix(p, f.seq - f.n), 4 * lane, 4, m, l, own);
 }
 
 // ---- many rows ------------------------------------------------------------------------------------------------------------
@@ -778,10 +783,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
     }
     const int rows = n * p.G, base = seq - n, r0 = f.tile * kTileRows + wv * kWaveRows, r = r0 + (lane & 31), hf = lane >> 5;
     const bool real = r < rows;
-    const int tok = real ? r / p.G : 0, head = h * p.G + (real ? r % p.G : 0);
+    const int tok = real ? token_of(p, r) : 0, head = h * p.G + (real ? r - tok * p.G : 0);
     const int pos = real ? base + tok : -1;
-    const int tmin = max(base + f.tile * kTileRows / p.G, 0), tmax = base + (min(f.tile * kTileRows + kTileRows, rows) - 1) / p.G;
-    const int pmin = max(base + r0 / p.G, 0), pmax = r0 < rows ? base + (min(r0 + kWaveRows, rows) - 1) / p.G : -1;    // of the wave's rows
+    const int tmin = max(base + token_of(p, f.tile * kTileRows), 0), tmax = base + token_of(p, min(f.tile * kTileRows + kTileRows, rows) - 1);
+    const int pmin = max(base + token_of(p, r0), 0), pmax = r0 < rows ? base + token_of(p, min(r0 + kWaveRows, rows) - 1) : -1;    // of the wave's rows
     bf16x8 q[D / 16];
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
@@ -929,9 +934,9 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_tiles_kernel(AttnParam
             o = o * a + u * e;
             m = top;
         }
-        const int ro = f.tile * kTileRows + row;
+        const int ro = f.tile * kTileRows + row, tok = token_of(p, ro);
         f32x4 own[1] = {o};
-        finish_row<D>(p, first + ro / p.G, h * p.G + ro % p.G, behind_prefix(p, seq - n), 4 * lane, 4, m, l, own);
+        finish_row<D>(p, first + tok, h * p.G + ro - tok * p.G, behind_prefix(p, seq - n), 4 * lane, 4, m, l, own);
     }
 }
 
@@ -1036,8 +1041,8 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
     const AttnSpace w = attention_space(T, G, KVH, D, prefix_len);
     const bool wide = w.wide && (int64_t)max_new * G > kNarrowRows;
     char *const ws = (char *)workspace;
-    AttnParams p = {q, k_cache, v_cache, block_table, q_start, seq_len, prefix_table, out, lse, q_stride, out_stride, B, T, KVH, QH / KVH,
-                    num_pages, max_pages, page_size, page_multiplier(page_size), scale * k_scale * kLog2e, v_scale,
+    AttnParams p = {q, k_cache, v_cache, block_table, q_start, seq_len, prefix_table, out, lse, q_stride, out_stride, B, T, KVH, G,
+                    num_pages, max_pages, page_size, page_multiplier(page_size), reciprocal(G), reciprocal(w.parts), scale * k_scale * kLog2e, v_scale,
                     window < kMaxContext ? window : 0, sinks < kMaxContext ? sinks : kMaxContext,   // (a window that long hides nothing)
                     w.parts, (float *)ws, (float *)(ws + w.ml_off), wide ? kNarrowRows : INT_MAX, w.wide_parts, (float *)(ws + w.wide_o_off),
                     (float *)(ws + w.wide_ml_off), prefix_len / kBlock, w.prefix_splits, (float *)(ws + w.prefix_o_off), (float *)(ws + w.prefix_ml_off),
