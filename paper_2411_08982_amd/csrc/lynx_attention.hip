@@ -243,14 +243,13 @@ struct Step {
     {
         const int kt = key_token(t0), vt = run_token(t0);
         const int kp = page_of(p, kt >> 4), vp = page_of(p, vt >> 4);
-        const bool kok = kp < p.max_pages && (unsigned)kid < (unsigned)p.num_pages;
+        const bool kok = (unsigned)kid < (unsigned)p.num_pages;
         vok = vp < p.max_pages && (unsigned)vid < (unsigned)p.num_pages;
         const size_t head_bytes = (size_t)p.page_size * D * E;
-        // (tokens without a page are read from the first page's start and not seen)
-        const uint8_t *ka = (const uint8_t *)p.k + ((size_t)(kok ? kid : 0) * p.KVH + h) * head_bytes + (kok ? kt - kp * p.page_size : 0) * (D * E) +
-                            (lane_id() >> 4) * 16;
+        // (tokens without a page are read from the first one and not seen)
+        const uint8_t *ka = (const uint8_t *)p.k + ((size_t)(kok ? kid : 0) * p.KVH + h) * head_bytes + (kt - kp * p.page_size) * (D * E) + (lane_id() >> 4) * 16;
         const uint8_t *va = (const uint8_t *)p.v + ((size_t)(vok ? vid : 0) * p.KVH + h) * head_bytes +
-                            (size_t)((lane_id() & 15) * p.page_size + (vok ? vt - vp * p.page_size : 0)) * E;
+                            (size_t)((lane_id() & 15) * p.page_size + vt - vp * p.page_size) * E;
 #pragma unroll
         for (int j = 0; j < NS; ++j)
 #pragma unroll
@@ -692,21 +691,25 @@ struct BlockLoad {
         vput = d * 8 + ((2 * wv + (F8 ? 0 : lane % VP)) ^ (d & 7));
     }
 
-    // Lane l: number of the page of the block's l % 4th 16 tokens, -1 if there is none.
+    // Lane l: what the table says of the page of the block's l % 4th 16 tokens, and whether there is such a page.  (Apart, for the
+    // number to be on its way until it is used.)
     static __device__ __forceinline__ int fetch_pages(const AttnParams &p, const int32_t *pages, int blk)
     {
-        const int idx = page_of(p, blk * (kBlock / 16) + (lane_id() & 3));
-        const int id = pages[min(idx, p.max_pages - 1)];
-        return idx < p.max_pages && (unsigned)id < (unsigned)p.num_pages ? id : -1;
+        return pages[min(page_of(p, blk * (kBlock / 16) + (lane_id() & 3)), p.max_pages - 1)];
+    }
+    static __device__ __forceinline__ bool valid(const AttnParams &p, int blk, int id)
+    {
+        return page_of(p, blk * (kBlock / 16) + (lane_id() & 3)) < p.max_pages && (unsigned)id < (unsigned)p.num_pages;
     }
 
+    // (tokens without a page are read from the first one)
     __device__ __forceinline__ void fetch(const AttnParams &p, int h, int wv, int blk, int ids)
     {
         const size_t head_bytes = (size_t)p.page_size * D * E;
+        const int known = (unsigned)ids < (unsigned)p.num_pages ? ids : 0;
         const auto group = [&](int g, const void *cache, int token_bytes) {
-            const int id = __builtin_amdgcn_readlane(ids, g), at = blk * (kBlock / 16) + g;
-            const int place = id < 0 ? 0 : at * 16 - page_of(p, at) * p.page_size;
-            return (const uint8_t *)cache + ((size_t)max(id, 0) * p.KVH + h) * head_bytes + (size_t)(place * token_bytes);
+            const int at = blk * (kBlock / 16) + g, place = at * 16 - page_of(p, at) * p.page_size;
+            return (const uint8_t *)cache + ((size_t)__builtin_amdgcn_readlane(known, g) * p.KVH + h) * head_bytes + (size_t)(place * token_bytes);
         };
 #pragma unroll
         for (int i = 0; i < KI; ++i)
@@ -717,10 +720,10 @@ struct BlockLoad {
     }
 
     // Values of tokens that no row of the tile sees become zero (they may be no numbers).
-    __device__ __forceinline__ void blank(const AttnParams &p, int wv, int blk, int ids, int pmin, int pmax)
+    __device__ __forceinline__ void blank(const AttnParams &p, int wv, int blk, unsigned pages, int pmin, int pmax)
     {
         const int t0 = blk * kBlock + 16 * wv + (F8 ? 0 : (int)(lane_id() % VP) * 8);
-        const bool ok = __builtin_amdgcn_readlane(ids, wv) >= 0;
+        const unsigned ok = pages >> wv & 1u;
         u32x4 mask;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -814,11 +817,11 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
     for (int i = i0; i < i1; ++i) {
         const int blk = blocks.at(i), t0 = blk * kBlock;
         // the block's values and keys into LDS, the next one's on their way, this one's products
-        const bool all_ok = __all(ids >= 0);
-        if (t0 + kBlock - 1 > tmax || !all_ok || (p.window != 0 && t0 <= tmin - p.window && t0 + kBlock > p.sinks)) next.blank(p, wv, blk, ids, tmin, tmax);
+        const unsigned there = (unsigned)__ballot(B::valid(p, blk, ids)) & 15u;      // which of its 16 tokens have a page
+        const bool all_ok = there == 15u;
+        if (t0 + kBlock - 1 > tmax || !all_ok || (p.window != 0 && t0 <= tmin - p.window && t0 + kBlock > p.sinks)) next.blank(p, wv, blk, there, tmin, tmax);
         u32x4 *kb = kbuf[(i - i0) & 1], *vb = vbuf[(i - i0) & 1];
         next.put(kb, vb);
-        const int now = ids;
         ids = ids_next;
         if (i + 1 < i1) {
             ids_next = B::fetch_pages(p, pages, blocks.at(min(i + 2, i1 - 1)));
@@ -827,16 +830,33 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
         __syncthreads();
         if (t0 > pmax || (p.window != 0 && t0 + kBlock - 1 <= pmin - p.window && t0 >= p.sinks)) continue;   // nothing for this wave
 
+        // Fragments are read ahead of their products: the second half's keys and the first values' beside products, the others'
+        // values beside the products of the first.
+        constexpr int NQ = D / 16, NV = D / 32;
+        const auto key = [&](int t, int j) { return __builtin_bit_cast(bf16x8, kb[(t * 32 + (lane & 31)) * (D / 8) + ((2 * j + hf) ^ (lane & 7))]); };
+        const auto value = [&](int t, int s) { return __builtin_bit_cast(bf16x8, vb[(t * 32 + (lane & 31)) * 8 + ((2 * s + hf) ^ (lane & 7))]); };
+        bf16x8 ka[2][NQ], va[2][4];
         f32x16 z[2];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int j = 0; j < NQ; ++j) ka[0][j] = key(0, j);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) z[t][j] = 0.0f;
+        for (int j = 0; j < 16; ++j) z[0][j] = z[1][j] = 0.0f;
 #pragma unroll
-            for (int j = 0; j < D / 16; ++j) {
-                const u32x4 a = kb[(t * 32 + (lane & 31)) * (D / 8) + ((2 * j + hf) ^ (lane & 7))];
-                z[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), q[j], z[t], 0, 0, 0);
-            }
+        for (int j = 0; j < NQ; ++j) {
+            ka[1][j] = key(1, j);
+            z[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[0][j], q[j], z[0], 0, 0, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) {
+            if (j < 4) va[0][j] = value(0, j);
+            else va[1][j - 4] = value(1, j - 4);
+            z[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[1][j], q[j], z[1], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x100, NQ, 0);
+#pragma unroll
+        for (int j = 0; j < 2 * NQ; ++j) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
         // lane: tokens t0 + 32 t + 16 (j / 8) + 8 hf + j % 8
         const bool in_window = p.window == 0 || t0 > pmax - p.window || t0 + kBlock <= p.sinks;
@@ -845,7 +865,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    const bool ok = __builtin_amdgcn_readlane(now, 2 * t + s) >= 0;
+                    const unsigned ok = there >> (2 * t + s) & 1u;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         const int at = t0 + 32 * t + 16 * s + 8 * hf + j;
@@ -882,11 +902,13 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
                 w[2 * t + s] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7])));
             }
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t)
+        for (int t = 0; t < NV; ++t)
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                const u32x4 a = vb[(t * 32 + (lane & 31)) * 8 + ((2 * s + hf) ^ (lane & 7))];
-                o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), w[s], o[t], 0, 0, 0);
+                const bf16x8 a = va[t & 1][s];
+                if (t == 0 && D == 64) va[1][s] = value(1, s);
+                else if (t + 2 < NV) va[t & 1][s] = value(t + 2, s);
+                o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w[s], o[t], 0, 0, 0);
             }
     }
     l = half_sum(l);
