@@ -665,11 +665,13 @@ __device__ __forceinline__ float half_sum(float v)
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// A block of 64 tokens on its way from the pages into LDS: 16 bytes per load and thread.  Each of the block's four groups of 16 tokens
-// lies in one page; what one load instruction brings is of one group, so that its address is a scalar and a constant of the lane.
-//   keys [64][D]: row m holds token 16 (m / 16) + (m % 16 with bits 2 and 3 exchanged), see attn_tiles_kernel;
-//   values [D][64]; wave w brings group w.  The 16-byte pieces of a row are stored at their place xor (row & 7): the lanes of a
-//   fragment read one column of pieces, which would all lie in the same banks.
+// A block of 64 tokens on its way from the pages into LDS, 16 bytes per load and lane.  Each of the block's four groups of 16 tokens lies
+// in one page; what one load instruction brings is of one group, so that its address is a scalar and a constant of the lane.
+//   keys [64][D]: row m holds token 16 (m / 16) + (m % 16 with bits 2 and 3 exchanged), see attn_tiles_kernel; the 16-byte pieces of
+//   a row stand at their place xor (m & 7);
+//   values [4 groups][D][2 pieces]: wave w brings group w; the two pieces of a channel change places where bit 2 of it is set.
+// (The lanes of a fragment read one column of pieces, which would all lie in the same banks.)
+// A bf16 block goes from memory to LDS directly; an 8-bit one is widened in registers on its way.
 template <int D, bool F8>
 struct BlockLoad {
     static constexpr int E = F8 ? 1 : 2;
@@ -677,18 +679,18 @@ struct BlockLoad {
     static constexpr int KI = kBlock * KP / kAttnThreads;
     static constexpr int VP = E;                                         // loads of a group of one channel
     static constexpr int VI = D * VP / kWave;
-    u32x4 kw[KI], vw[VI];
-    unsigned koff, voff;          // the lane's places in a group of keys and of values (bytes), and in LDS (16-byte pieces)
-    int kput, vput;
+    u32x4 kw[F8 ? KI : 1], vw[F8 ? VI : 1];
+    unsigned koff, voff;          // the lane's places in a group of keys and of values (bytes)
+    int kput, vput;               // and, of an 8-bit block, in LDS (16-byte pieces)
 
     __device__ __forceinline__ BlockLoad(const AttnParams &p)
     {
-        const int tid = threadIdx.x, lane = lane_id(), wv = wave_id();
-        const int m = tid / KP, r = m & 15, tok = (r & 3) | (r & 4) << 1 | (r & 8) >> 1, d = lane / VP;
-        koff = (unsigned)(tok * (D * E) + tid % KP * 16);
-        voff = (unsigned)(d * p.page_size + lane % VP * 8) * E;
-        kput = m * (D / 8) + ((tid % KP * (2 / E)) ^ (m & 7));
-        vput = d * 8 + ((2 * wv + (F8 ? 0 : lane % VP)) ^ (d & 7));
+        const int tid = threadIdx.x, lane = lane_id();
+        const int m = tid / KP, r = m & 15, tok = (r & 3) | (r & 4) << 1 | (r & 8) >> 1, d = lane / VP, swap = d >> 2 & 1;
+        koff = (unsigned)(tok * (D * E) + (F8 ? tid % KP : (tid % KP) ^ (m & 7)) * 16);
+        voff = (unsigned)(d * p.page_size + (F8 ? 0 : ((lane & 1) ^ swap) * 8)) * E;
+        kput = m * (D / 8) + ((2 * (tid % KP)) ^ (m & 7));
+        vput = (wave_id() * D + d) * 2 + swap;
     }
 
     // Lane l: what the table says of the page of the block's l % 4th 16 tokens, and whether there is such a page.  (Apart, for the
@@ -697,80 +699,104 @@ struct BlockLoad {
     {
         return pages[min(page_of(p, blk * (kBlock / 16) + (lane_id() & 3)), p.max_pages - 1)];
     }
-    static __device__ __forceinline__ bool valid(const AttnParams &p, int blk, int id)
+    static __device__ __forceinline__ unsigned there(const AttnParams &p, int blk, int id)      // bit g: group g has a page
     {
-        return page_of(p, blk * (kBlock / 16) + (lane_id() & 3)) < p.max_pages && (unsigned)id < (unsigned)p.num_pages;
+        return (unsigned)__ballot(page_of(p, blk * (kBlock / 16) + (lane_id() & 3)) < p.max_pages && (unsigned)id < (unsigned)p.num_pages) & 15u;
     }
 
-    // (tokens without a page are read from the first one)
-    __device__ __forceinline__ void fetch(const AttnParams &p, int h, int wv, int blk, int ids)
+    // Where group g of the block begins in the keys or values of head h.  (Tokens without a page are read from the first one.)
+    static __device__ __forceinline__ const uint8_t *group(const AttnParams &p, const void *cache, int token_bytes, int h, int blk, int ids, int g)
     {
-        const size_t head_bytes = (size_t)p.page_size * D * E;
-        const int known = (unsigned)ids < (unsigned)p.num_pages ? ids : 0;
-        const auto group = [&](int g, const void *cache, int token_bytes) {
-            const int at = blk * (kBlock / 16) + g, place = at * 16 - page_of(p, at) * p.page_size;
-            return (const uint8_t *)cache + ((size_t)__builtin_amdgcn_readlane(known, g) * p.KVH + h) * head_bytes + (size_t)(place * token_bytes);
-        };
-#pragma unroll
-        for (int i = 0; i < KI; ++i)
-            kw[i] = *reinterpret_cast<const u32x4 *>(group((i * kAttnThreads + wv * kWave) / (16 * KP), p.k, D * E) + koff);
-        const uint8_t *va = group(wv, p.v, E);
-#pragma unroll
-        for (int i = 0; i < VI; ++i) vw[i] = *reinterpret_cast<const u32x4 *>(va + (size_t)i * (kWave / VP) * p.page_size * E + voff);
+        const int id = __builtin_amdgcn_readlane(ids, g), at = blk * (kBlock / 16) + g, place = at * 16 - page_of(p, at) * p.page_size;
+        return (const uint8_t *)cache + ((size_t)((unsigned)id < (unsigned)p.num_pages ? id : 0) * p.KVH + h) * ((size_t)p.page_size * D * E) +
+               (size_t)(place * token_bytes);
+    }
+    static __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const uint8_t *base)
+    {
+        const unsigned long long a = reinterpret_cast<unsigned long long>(base);
+        const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)a), hi = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));
+        return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(((unsigned long long)hi << 32) | lo), 0, 0x7fffffff, 0x00020000);
     }
 
-    // Values of tokens that no row of the tile sees become zero (they may be no numbers).
-    __device__ __forceinline__ void blank(const AttnParams &p, int wv, int blk, unsigned pages, int pmin, int pmax)
+    __device__ __forceinline__ void keys(const AttnParams &p, int h, int wv, int blk, int ids, u32x4 *kb)
     {
-        const int t0 = blk * kBlock + 16 * wv + (F8 ? 0 : (int)(lane_id() % VP) * 8);
-        const unsigned ok = pages >> wv & 1u;
+#pragma unroll
+        for (int i = 0; i < KI; ++i) {
+            const uint8_t *src = group(p, p.k, D * E, h, blk, ids, (i * kAttnThreads + wv * kWave) / (16 * KP));
+            if constexpr (F8) kw[i] = *reinterpret_cast<const u32x4 *>(src + koff);
+            else __builtin_amdgcn_raw_ptr_buffer_load_lds(resource(src), (__attribute__((address_space(3))) void *)(kb + i * kAttnThreads + wv * kWave), 16, koff, 0, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void values(const AttnParams &p, int h, int wv, int blk, int ids, u32x4 *vb)
+    {
+        const uint8_t *src = group(p, p.v, E, h, blk, ids, wv);
+        const __amdgpu_buffer_rsrc_t rs = resource(src);
+#pragma unroll
+        for (int i = 0; i < VI; ++i) {
+            const int next = i * (kWave / VP) * p.page_size * E;
+            if constexpr (F8) vw[i] = *reinterpret_cast<const u32x4 *>(src + next + voff);
+            else __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)(vb + wv * D * 2 + i * kWave), 16, voff, next, 0, 0);
+        }
+    }
+
+    // The lane's values that no row of the tile sees (they may be no numbers) as a mask of zeros.
+    __device__ __forceinline__ u32x4 hidden(const AttnParams &p, int wv, int blk, unsigned there, int pmin, int pmax) const
+    {
+        const int t0 = blk * kBlock + 16 * wv + (F8 ? 0 : (int)((lane_id() & 1) ^ (lane_id() >> 3 & 1)) * 8);
         u32x4 mask;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             mask[w] = 0u;
 #pragma unroll
-            for (int i = 0; i < 4 / E; ++i) {
-                const int any = (int)ok & seen(p, t0 + w * (4 / E) + i, pmin, pmax);
-                mask[w] |= any ? (F8 ? 0xffu << (8 * i) : 0xffffu << (16 * i)) : 0u;
-            }
+            for (int i = 0; i < 4 / E; ++i)
+                mask[w] |= (int)(there >> wv & 1u) & seen(p, t0 + w * (4 / E) + i, pmin, pmax) ? (F8 ? 0xffu << (8 * i) : 0xffffu << (16 * i)) : 0u;
         }
-#pragma unroll
-        for (int i = 0; i < VI; ++i) vw[i] &= mask;
+        return mask;
     }
 
-    __device__ __forceinline__ void put(u32x4 *kb, u32x4 *vb) const
+    __device__ __forceinline__ void put_keys(u32x4 *kb) const
     {
 #pragma unroll
         for (int i = 0; i < KI; ++i) {
-            u32x4 *dst = kb + kput + i * (kAttnThreads / KP) * (D / 8);
-            if (F8) {
-                dst[0] = __builtin_bit_cast(u32x4, widen8(make_uint2(kw[i].x, kw[i].y)));
-                kb[(kput ^ 1) + i * (kAttnThreads / KP) * (D / 8)] = __builtin_bit_cast(u32x4, widen8(make_uint2(kw[i].z, kw[i].w)));
-            } else {
-                dst[0] = kw[i];
-            }
+            kb[kput + i * (kAttnThreads / KP) * (D / 8)] = __builtin_bit_cast(u32x4, widen8(make_uint2(kw[i].x, kw[i].y)));
+            kb[(kput ^ 1) + i * (kAttnThreads / KP) * (D / 8)] = __builtin_bit_cast(u32x4, widen8(make_uint2(kw[i].z, kw[i].w)));
         }
+    }
+    __device__ __forceinline__ void put_values(u32x4 *vb) const
+    {
 #pragma unroll
         for (int i = 0; i < VI; ++i) {
-            u32x4 *dst = vb + vput + i * (kWave / VP) * 8;
-            if (F8) {
-                dst[0] = __builtin_bit_cast(u32x4, widen8(make_uint2(vw[i].x, vw[i].y)));
-                vb[(vput ^ 1) + i * (kWave / VP) * 8] = __builtin_bit_cast(u32x4, widen8(make_uint2(vw[i].z, vw[i].w)));
-            } else {
-                dst[0] = vw[i];
-            }
+            vb[vput + i * kWave * 2] = __builtin_bit_cast(u32x4, widen8(make_uint2(vw[i].x, vw[i].y)));
+            vb[(vput ^ 1) + i * kWave * 2] = __builtin_bit_cast(u32x4, widen8(make_uint2(vw[i].z, vw[i].w)));
         }
     }
 };
 
+// Everything that this wave has asked for has come, and every wave is here: what the waves brought into LDS is there for all.  (Written
+// out, since a load into LDS is no write that a barrier would wait for.)
+__device__ __forceinline__ void blocks_ready()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// A turn of the loop has the second product of one block and the first of the next, whose matrix instructions stand between the VALU
+// instructions of the softmax.  In LDS at a turn's start: its values and the next keys; on their way during it: the next values and
+// the keys after next.
 // PREFIX: the rows are those of the whole batch, whatever request they belong to, and the context is the shared prefix's whole blocks,
 // which all of them see; every row's part is left in the workspace.
 template <int D, bool F8, bool PREFIX>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams p)
 {
     typedef BlockLoad<D, F8> B;
-    __shared__ FindShared sh;
-    __shared__ __align__(16) u32x4 kbuf[2][kBlock * D / 8], vbuf[2][kBlock * D / 8];
+    constexpr int NQ = D / 16, NV = D / 32, kAhead = 4;     // fragments are read from LDS four products ahead
+    // Four arrays and nothing else: loads into LDS reach its first 64 KiB, and which of two buffers is meant has to be known when
+    // this is compiled, for a read of one not to wait for loads into the other.
+    __shared__ __align__(16) u32x4 kbuf0[kBlock * D / 8], vbuf0[kBlock * D / 8], kbuf1[kBlock * D / 8], vbuf1[kBlock * D / 8];
+    static_assert(sizeof(FindShared) <= sizeof kbuf0 && 4 * sizeof kbuf0 <= 65536, "LDS");
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id()), h = blockIdx.y;
     constexpr int kFar = 1 << 30;                   // behind every token of a prefix
     Part f;
@@ -781,8 +807,9 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
         n = p.T;
         seq = kFar + p.T;
     } else {
-        if (!find_part<false>(p, blockIdx.x, sh, f)) return;
+        if (!find_part<false>(p, blockIdx.x, *reinterpret_cast<FindShared *>(kbuf0), f)) return;
         request_of(p, f.b, first, n, seq);
+        __syncthreads();                            // kbuf0 is free again
     }
     const int rows = n * p.G, base = seq - n, r0 = f.tile * kTileRows + wv * kWaveRows, r = r0 + (lane & 31), hf = lane >> 5;
     const bool real = r < rows;
@@ -790,77 +817,115 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
     const int pos = real ? base + tok : -1;
     const int tmin = max(base + token_of(p, f.tile * kTileRows), 0), tmax = base + token_of(p, min(f.tile * kTileRows + kTileRows, rows) - 1);
     const int pmin = max(base + token_of(p, r0), 0), pmax = r0 < rows ? base + token_of(p, min(r0 + kWaveRows, rows) - 1) : -1;    // of the wave's rows
-    bf16x8 q[D / 16];
+    const Blocks blocks = PREFIX ? Blocks{0, 0, p.prefix_blocks} : blocks_of(p, base, tmin, tmax);
+    const int per = (blocks.count + f.splits - 1) / f.splits, i0 = f.split * per, i1 = min(i0 + per, blocks.count);
+    const int32_t *pages = PREFIX ? p.prefix_table : p.table + (size_t)f.b * p.max_pages;
+    const auto block = [&](int i) { return blocks.at(min(i, i1 - 1)); };
+
+    B load(p);
+    int id1 = 0, id2 = 0, id3 = 0;                  // page numbers of the next blocks
+    unsigned there = 15u;                           // which groups of this turn's block have a page
+    if (i0 < i1) {
+        const int id0 = B::fetch_pages(p, pages, block(i0));
+        id1 = B::fetch_pages(p, pages, block(i0 + 1));
+        id2 = B::fetch_pages(p, pages, block(i0 + 2));
+        if (F8) id3 = B::fetch_pages(p, pages, block(i0 + 3));
+        there = B::there(p, block(i0), id0);
+        load.keys(p, h, wv, block(i0), id0, kbuf0);
+        load.values(p, h, wv, block(i0), id0, vbuf0);
+    }
+    bf16x8 q[NQ];
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
+    for (int i = 0; i < NQ; ++i) {
         u32x4 u = {0u, 0u, 0u, 0u};
         if (real) u = *reinterpret_cast<const u32x4 *>(p.q + (size_t)(first + tok) * p.q_stride + (size_t)head * D + i * 16 + hf * 8);
         q[i] = __builtin_bit_cast(bf16x8, u);
     }
     float m = -INFINITY, l = 0.0f;
-    f32x16 o[D / 32];
+    f32x16 o[NV];
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t)
+    for (int t = 0; t < NV; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
 
-    const Blocks blocks = PREFIX ? Blocks{0, 0, p.prefix_blocks} : blocks_of(p, base, tmin, tmax);
-    const int per = (blocks.count + f.splits - 1) / f.splits, i0 = f.split * per, i1 = min(i0 + per, blocks.count);
-    const int32_t *pages = PREFIX ? p.prefix_table : p.table + (size_t)f.b * p.max_pages;
-    B next(p);
-    int ids = 0, ids_next = 0;
+    const int krow = (lane & 31) * (D / 8), vrow = (lane & 31) * 2 + (hf ^ (lane >> 2 & 1));
+    const auto key = [&](const u32x4 *kb, int i) {      // fragment i of the 2 NQ, of 32 tokens' keys after the other
+        return __builtin_bit_cast(bf16x8, kb[i / NQ * 32 * (D / 8) + krow + ((2 * (i % NQ) + hf) ^ (lane & 7))]);
+    };
+    const auto value = [&](const u32x4 *vb, int i) {     // fragment i of the 4 NV: 16 tokens after 16 tokens
+        return __builtin_bit_cast(bf16x8, vb[(i / NV * D + i % NV * 32) * 2 + vrow]);
+    };
+    const auto partly = [&](int blk, unsigned t) {        // some of the block's tokens are seen by no row of the tile
+        const int t0 = blk * kBlock;
+        return t != 15u || t0 + kBlock - 1 > tmax || (p.window != 0 && t0 <= tmin - p.window && t0 + kBlock > p.sinks);
+    };
+    f32x16 za[2], zb[2];
     if (i0 < i1) {
-        ids = B::fetch_pages(p, pages, blocks.at(i0));
-        ids_next = B::fetch_pages(p, pages, blocks.at(min(i0 + 1, i1 - 1)));
-        next.fetch(p, h, wv, blocks.at(i0), ids);
+        if constexpr (F8) {
+            if (partly(block(i0), there)) {
+                const u32x4 mask = load.hidden(p, wv, block(i0), there, tmin, tmax);
+#pragma unroll
+                for (int i = 0; i < B::VI; ++i) load.vw[i] &= mask;
+            }
+            load.put_keys(kbuf0);
+            load.put_values(vbuf0);
+            load.keys(p, h, wv, block(i0 + 1), id1, kbuf1);
+            load.put_keys(kbuf1);
+            load.values(p, h, wv, block(i0 + 1), id1, vbuf1);
+            load.keys(p, h, wv, block(i0 + 2), id2, kbuf0);
+        } else {
+            load.keys(p, h, wv, block(i0 + 1), id1, kbuf1);
+        }
+        blocks_ready();
+        bf16x8 ka[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) ka[i] = key(kbuf0, i);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) za[0][i] = za[1][i] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 2 * NQ; ++i) {
+            const bf16x8 a = ka[i % kAhead];
+            if (i + kAhead < 2 * NQ) ka[i % kAhead] = key(kbuf0, i + kAhead);
+            za[i / NQ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[i % NQ], za[i / NQ], 0, 0, 0);
+        }
     }
-    for (int i = i0; i < i1; ++i) {
-        const int blk = blocks.at(i), t0 = blk * kBlock;
-        // the block's values and keys into LDS, the next one's on their way, this one's products
-        const unsigned there = (unsigned)__ballot(B::valid(p, blk, ids)) & 15u;      // which of its 16 tokens have a page
-        const bool all_ok = there == 15u;
-        if (t0 + kBlock - 1 > tmax || !all_ok || (p.window != 0 && t0 <= tmin - p.window && t0 + kBlock > p.sinks)) next.blank(p, wv, blk, there, tmin, tmax);
-        u32x4 *kb = kbuf[(i - i0) & 1], *vb = vbuf[(i - i0) & 1];
-        next.put(kb, vb);
-        ids = ids_next;
-        if (i + 1 < i1) {
-            ids_next = B::fetch_pages(p, pages, blocks.at(min(i + 2, i1 - 1)));
-            next.fetch(p, h, wv, blocks.at(i + 1), ids);
+    // kn, vn: this turn's keys, whose buffer is free, and values; kx, vx: the next ones'
+    const auto turn = [&](int i, u32x4 *kn, u32x4 *vn, u32x4 *kx, u32x4 *vx, f32x16 (&z)[2], f32x16 (&zn)[2]) {
+        const int blk = block(i), t0 = blk * kBlock, blk1 = block(i + 1), blk2 = block(i + 2);
+        const unsigned there1 = B::there(p, blk1, id1);
+        blocks_ready();
+        if constexpr (F8) {
+            if (partly(blk1, there1)) {
+                const u32x4 mask = load.hidden(p, wv, blk1, there1, tmin, tmax);
+#pragma unroll
+                for (int j = 0; j < B::VI; ++j) load.vw[j] &= mask;
+            }
+            load.put_values(vx);
+            load.put_keys(kn);
+            load.values(p, h, wv, blk2, id2, vn);
+            load.keys(p, h, wv, block(i + 3), id3, kx);
+            id1 = id2;
+            id2 = id3;
+            id3 = B::fetch_pages(p, pages, block(i + 4));
+        } else {
+            if (partly(blk, there)) {
+                const u32x4 mask = load.hidden(p, wv, blk, there, tmin, tmax);
+#pragma unroll
+                for (int j = 0; j < B::VI; ++j) vn[wv * D * 2 + j * kWave + lane] &= mask;
+                blocks_ready();
+            }
+            load.values(p, h, wv, blk1, id1, vx);
+            load.keys(p, h, wv, blk2, id2, kn);
+            id1 = id2;
+            id2 = B::fetch_pages(p, pages, block(i + 3));
         }
-        __syncthreads();
-        if (t0 > pmax || (p.window != 0 && t0 + kBlock - 1 <= pmin - p.window && t0 >= p.sinks)) continue;   // nothing for this wave
-
-        // Fragments are read ahead of their products: the second half's keys and the first values' beside products, the others'
-        // values beside the products of the first.
-        constexpr int NQ = D / 16, NV = D / 32;
-        const auto key = [&](int t, int j) { return __builtin_bit_cast(bf16x8, kb[(t * 32 + (lane & 31)) * (D / 8) + ((2 * j + hf) ^ (lane & 7))]); };
-        const auto value = [&](int t, int s) { return __builtin_bit_cast(bf16x8, vb[(t * 32 + (lane & 31)) * 8 + ((2 * s + hf) ^ (lane & 7))]); };
-        bf16x8 ka[2][NQ], va[2][4];
-        f32x16 z[2];
+        __builtin_amdgcn_sched_barrier(0);
+        bf16x8 ka[kAhead], va[kAhead];
 #pragma unroll
-        for (int j = 0; j < NQ; ++j) ka[0][j] = key(0, j);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) z[0][j] = z[1][j] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < NQ; ++j) {
-            ka[1][j] = key(1, j);
-            z[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[0][j], q[j], z[0], 0, 0, 0);
-        }
-#pragma unroll
-        for (int j = 0; j < NQ; ++j) {
-            if (j < 4) va[0][j] = value(0, j);
-            else va[1][j - 4] = value(1, j - 4);
-            z[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[1][j], q[j], z[1], 0, 0, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x100, NQ, 0);
-#pragma unroll
-        for (int j = 0; j < 2 * NQ; ++j) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
+        for (int j = 0; j < kAhead; ++j) ka[j] = key(kx, j);
         // lane: tokens t0 + 32 t + 16 (j / 8) + 8 hf + j % 8
         const bool in_window = p.window == 0 || t0 > pmax - p.window || t0 + kBlock <= p.sinks;
-        if (!(t0 + kBlock - 1 <= pmin && in_window && all_ok)) {
+        if (!(t0 + kBlock - 1 <= pmin && in_window && there == 15u)) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -873,44 +938,59 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
                     }
                 }
         }
+        there = there1;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) zn[0][j] = zn[1][j] = 0.0f;
+        const auto first_product = [&](int j) {
+            const bf16x8 a = ka[j % kAhead];
+            if (j + kAhead < 2 * NQ) ka[j % kAhead] = key(kx, j + kAhead);
+            zn[j / NQ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[j % NQ], zn[j / NQ], 0, 0, 0);
+        };
+        constexpr int kBefore = NQ / 2;         // products beside the maximum
         float top = z[0][0];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int j = 0; j < 16; ++j) top = fmaxf(top, z[t][j]);
+#pragma unroll
+        for (int j = 0; j < kBefore; ++j) first_product(j);
         top = half_max(top) * p.scale2;
         // m follows the maximum only when it is 8 behind: until then weights are up to 2^8, and rows are rescaled less often
         if (__any(top > m + 8.0f)) {
             const float up = fmaxf(m, top), a = up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - up);
             l *= a;
 #pragma unroll
-            for (int t = 0; t < D / 32; ++t) o[t] *= a;
+            for (int t = 0; t < NV; ++t) o[t] *= a;
             m = up;
         }
         const float off = m == -INFINITY ? 0.0f : -m;
+#pragma unroll
+        for (int j = kBefore; j < 2 * NQ; ++j) first_product(j);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) va[j] = value(vn, j);
         bf16x8 w[4];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int s = 0; s < 4; ++s) {
+            float e[8];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                float e[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][s * 8 + j], p.scale2, off));
-                    l += e[j];
-                }
-                w[2 * t + s] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7])));
+            for (int j = 0; j < 8; ++j) {
+                e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[s / 2][s % 2 * 8 + j], p.scale2, off));
+                l += e[j];
             }
+            w[s] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7])));
+        }
 #pragma unroll
-        for (int t = 0; t < NV; ++t)
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const bf16x8 a = va[t & 1][s];
-                if (t == 0 && D == 64) va[1][s] = value(1, s);
-                else if (t + 2 < NV) va[t & 1][s] = value(t + 2, s);
-                o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w[s], o[t], 0, 0, 0);
-            }
+        for (int j = 0; j < 4 * NV; ++j) {
+            const bf16x8 a = va[j % kAhead];
+            if (j + kAhead < 4 * NV) va[j % kAhead] = value(vn, j + kAhead);
+            o[j % NV] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w[j / NV], o[j % NV], 0, 0, 0);
+        }
+    };
+    for (int i = i0; i < i1; i += 2) {
+        turn(i, kbuf0, vbuf0, kbuf1, vbuf1, za, zb);
+        if (i + 1 < i1) turn(i + 1, kbuf1, vbuf1, kbuf0, vbuf0, zb, za);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // nothing on its way into LDS when the workgroup ends
     l = half_sum(l);
     if (!real) return;
     // lane: channels 32 t + 8 j + 4 hf .. + 3 of its row
