@@ -504,9 +504,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_rows_kernel(AttnParams p
 
 // Joins the parts of the tiles that are cut.  Workgroup x has the x-th cut of the line; where it is the first that goes through a
 // tile, it joins the tile.  Few rows with many parts each are the case that counts (one request alone: a few rows, dozens of
-// parts), so a tile's rows are spread over kJoinSlices workgroups, and the parts of a row over what is left of the workgroup's
-// D / 4-lane groups, which meet in LDS.
-constexpr int kJoinSlices = 4;
+// parts), so there a tile's rows are spread over several workgroups, and the parts of a row over what is left of the workgroup's D / 4-lane
+// groups, which meet in LDS.
 template <int D>
 __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p)
 {
@@ -518,47 +517,52 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p)
     if (cut >= total) return;
     const Place f = place_of(p, line, cut);
     if (f.begin == cut || f.begin + length < cut) return;          // between two tiles, or not the first cut of this one
-    const int h = blockIdx.y, slice = blockIdx.z, here = min(f.n * p.G - f.tile * kRows, kRows);   // the tile's rows
-    const int mine = (here - slice + kJoinSlices - 1) / kJoinSlices;                               // those of this workgroup
-    if (mine <= 0) return;
-    const int width = mine > 2 ? 4 : mine;                                                         // (a power of two)
-    const int grp = threadIdx.x / L, lane = threadIdx.x % L, k = grp % width, sub = grp / width;
-    const int orow = slice + k * kJoinSlices;
-    const bool real = k < mine;
+    const int h = blockIdx.y, slice = blockIdx.z, slices = gridDim.z, here = min(f.n * p.G - f.tile * kRows, kRows);
+    const int mine = (here - slice + slices - 1) / slices;        // of the tile's rows, those of this workgroup
     const int parts = (int)((f.begin + f.count - 1) / length) - (int)blockIdx.x + 1;
-    float m = -INFINITY, l = 0.0f;
-    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int grp = threadIdx.x / L, lane = threadIdx.x % L;
+    for (int done = 0; done < mine; done += NG) {
+        int width = 1;                                              // rows at a time: a power of two
+        while (width < mine - done && width < NG) width *= 2;
+        const int k = done + grp % width, sub = grp / width, orow = slice + k * slices;
+        const bool real = k < mine;
+        float m = -INFINITY, l = 0.0f;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-    for (int i = sub; i < parts; i += NG / width) {
-        // the first part is the last of its workgroup unless the tile begins where the workgroup does
-        const unsigned x = blockIdx.x + i;
-        const size_t part = ((size_t)(2 * x + (f.begin >= x * length ? 1 : 0)) * p.KVH + h) * kRows + (real ? orow : slice);
-        const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * part);
-        const f32x4 u = *reinterpret_cast<const f32x4 *>(p.part_o + part * D + 4 * lane);
-        const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.0f : top;
-        const float a = __builtin_amdgcn_exp2f(m - base), e = __builtin_amdgcn_exp2f(ml.x - base);
-        l = l * a + e * ml.y;
-        o = o * a + u * e;
-        m = top;
+        for (int i = sub; i < parts; i += NG / width) {
+            // the first part is the last of its workgroup unless the tile begins where the workgroup does
+            const unsigned x = blockIdx.x + i;
+            const size_t part = ((size_t)(2 * x + (f.begin >= x * length ? 1 : 0)) * p.KVH + h) * kRows + (real ? orow : slice);
+            const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * part);
+            const f32x4 u = *reinterpret_cast<const f32x4 *>(p.part_o + part * D + 4 * lane);
+            const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.0f : top;
+            const float a = __builtin_amdgcn_exp2f(m - base), e = __builtin_amdgcn_exp2f(ml.x - base);
+            l = l * a + e * ml.y;
+            o = o * a + u * e;
+            m = top;
+        }
+        if (width < NG) {
+            if (lane == 0) {
+                sm[grp] = m;
+                sl[grp] = l;
+            }
+            so[grp][lane] = make_float4(o[0], o[1], o[2], o[3]);
+            __syncthreads();
+            for (int w = grp + width; sub == 0 && w < NG; w += width) {
+                const float4 u = so[w][lane];
+                const float top = fmaxf(m, sm[w]), base = top == -INFINITY ? 0.0f : top;
+                const float a = __builtin_amdgcn_exp2f(m - base), e = __builtin_amdgcn_exp2f(sm[w] - base);
+                l = l * a + e * sl[w];
+                o = o * a + f32x4{u.x, u.y, u.z, u.w} * e;
+                m = top;
+            }
+            __syncthreads();
+        }
+        if (sub != 0 || !real) continue;
+        const int ro = f.tile * kRows + orow, tok = token_of(p, ro);
+        f32x4 own[1] = {o};
+        finish_row<D>(p, f.first + tok, h * p.G + ro - tok * p.G, behind_prefix(p, f.seq - f.n), 4 * lane, 4, m, l, own);
     }
-    if (lane == 0) {
-        sm[grp] = m;
-        sl[grp] = l;
-    }
-    so[grp][lane] = make_float4(o[0], o[1], o[2], o[3]);
-    __syncthreads();
-    if (sub != 0 || !real) return;
-    for (int w = k + width; w < NG; w += width) {
-        const float4 u = so[w][lane];
-        const float top = fmaxf(m, sm[w]), base = top == -INFINITY ? 0.0f : top;
-        const float a = __builtin_amdgcn_exp2f(m - base), e = __builtin_amdgcn_exp2f(sm[w] - base);
-        l = l * a + e * sl[w];
-        o = o * a + f32x4{u.x, u.y, u.z, u.w} * e;
-        m = top;
-    }
-    const int ro = f.tile * kRows + orow, tok = token_of(p, ro);
-    f32x4 own[1] = {o};
-    finish_row<D>(p, f.first + tok, h * p.G + ro - tok * p.G, behind_prefix(p, f.seq - f.n), 4 * lane, 4, m, l, own);
 }
 
 // ---- many rows ------------------------------------------------------------------------------------------------------------
@@ -783,6 +787,8 @@ __device__ __forceinline__ void blocks_ready()
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// Workgroups go round the eight XCDs, each with an L2 of its own, and the key heads go round fastest: the tiles of one head, which read
+// the same keys and values, meet in few L2s (prompt chunks with 8 key heads: 378 us with the heads slowest, 299 so).
 // A turn of the loop has the second product of one block and the first of the next, whose matrix instructions stand between the VALU
 // instructions of the softmax.  In LDS at a turn's start: its values and the next keys; on their way during it: the next values and
 // the keys after next.
@@ -797,17 +803,17 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
     // this is compiled, for a read of one not to wait for loads into the other.
     __shared__ __align__(16) u32x4 kbuf0[kBlock * D / 8], vbuf0[kBlock * D / 8], kbuf1[kBlock * D / 8], vbuf1[kBlock * D / 8];
     static_assert(sizeof(FindShared) <= sizeof kbuf0 && 4 * sizeof kbuf0 <= 65536, "LDS");
-    const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id()), h = blockIdx.y;
+    const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id()), h = blockIdx.x % p.KVH, x = blockIdx.x / p.KVH;
     constexpr int kFar = 1 << 30;                   // behind every token of a prefix
     Part f;
     int first, n, seq;
     if (PREFIX) {
-        f = {0, (int)blockIdx.x / p.prefix_splits, (int)blockIdx.x % p.prefix_splits, p.prefix_splits, 0};
+        f = {0, x / p.prefix_splits, x % p.prefix_splits, p.prefix_splits, 0};
         first = 0;
         n = p.T;
         seq = kFar + p.T;
     } else {
-        if (!find_part<false>(p, blockIdx.x, *reinterpret_cast<FindShared *>(kbuf0), f)) return;
+        if (!find_part<false>(p, x, *reinterpret_cast<FindShared *>(kbuf0), f)) return;
         request_of(p, f.b, first, n, seq);
         __syncthreads();                            // kbuf0 is free again
     }
@@ -1011,7 +1017,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
 }
 
 // Joins the parts of the tiles of attn_tiles_kernel that are cut: D / 4 lanes to a row.
-constexpr int kTileSlices = 8;
+constexpr int kTileSlices = 4;
 template <int D>
 __global__ __launch_bounds__(kAttnThreads) void attn_join_tiles_kernel(AttnParams p)
 {
@@ -1155,20 +1161,23 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
     if (p.prefix_blocks > 0) {
         auto prefix_kernel = D == 128 ? (f8 ? attn_tiles_kernel<128, true, true> : attn_tiles_kernel<128, false, true>)
                                       : (f8 ? attn_tiles_kernel<64, true, true> : attn_tiles_kernel<64, false, true>);
-        hipLaunchKernelGGL(prefix_kernel, dim3(w.prefix_tiles * w.prefix_splits, KVH), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
+        hipLaunchKernelGGL(prefix_kernel, dim3((unsigned)KVH * w.prefix_tiles * w.prefix_splits), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
     }
     if (wide) {
         // tiles: sum of ceil(rows / 128) over requests of more than kNarrowRows rows
         const int tiles = (int)((int64_t)T * G / kTileRows) + (int)std::min<int64_t>(B, (int64_t)T * G / kNarrowRows);
         auto tiles_kernel = D == 128 ? (f8 ? attn_tiles_kernel<128, true, false> : attn_tiles_kernel<128, false, false>)
                                      : (f8 ? attn_tiles_kernel<64, true, false> : attn_tiles_kernel<64, false, false>);
-        hipLaunchKernelGGL(tiles_kernel, dim3(tiles + w.wide_parts, KVH), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
+        hipLaunchKernelGGL(tiles_kernel, dim3((unsigned)KVH * (tiles + w.wide_parts)), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
         hipLaunchKernelGGL((D == 128 ? attn_join_tiles_kernel<128> : attn_join_tiles_kernel<64>), dim3(std::min(tiles, w.wide_parts), KVH, kTileSlices),
                            dim3(kAttnThreads), 0, (hipStream_t)stream, p);
     }
     hipLaunchKernelGGL(kernel, dim3(w.parts, KVH), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
+    // a request's parts are w.parts / B on average: where they are many, a tile's rows go to four workgroups (one request of 9001 tokens:
+    // 15 -> 4.4 us); else to one, since most workgroups have nothing to join (64 requests: 6.3 -> 4.9 us)
+    const int slices = std::max(1, std::min(4, w.parts / (2 * B)));
     if (w.parts > 1)
-        hipLaunchKernelGGL((D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>), dim3(w.parts - 1, KVH, kJoinSlices), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
+        hipLaunchKernelGGL((D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>), dim3(w.parts - 1, KVH, slices), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
     if (p.prefix_blocks > 0)
         hipLaunchKernelGGL((D == 128 ? attn_finish_kernel<128> : attn_finish_kernel<64>), dim3((unsigned)(((int64_t)T * QH * (D / 4) + kAttnThreads - 1) / kAttnThreads)),
                            dim3(kAttnThreads), 0, (hipStream_t)stream, p);
