@@ -214,99 +214,129 @@ struct RowState {
     f32x4 o[D / 16];
 };
 
-// One step of TN tokens from token t0 on (t0 a multiple of TN), in three parts so that the next step's loads can be under way while
-// this one's products run: page numbers, keys and values, products.
+// A block of 64 tokens, in parts so that the next block's loads are under way while this one's products run: page numbers, keys, first
+// product; values, softmax and second product.
+// A bf16 block is two halves of 32 tokens, an 8-bit block is one piece: 16 bytes of a channel are 8 or 16 tokens of each of the four
+// lanes of a row.  Both halves' values are asked for together: with pages of 64 tokns they are the two halves of the same cache lines, and
+// asked for a step apart each line was read twice (256 requests of 1600 tokens, pages of 64: 3.5 TB/s).
 template <int D, bool F8>
 struct Step {
     static constexpr int E = F8 ? 1 : 2;           // bytes of an element
-    static constexpr int TN = F8 ? 64 : 32;        // tokens: 16 bytes of a channel from every lane
-    static constexpr int NS = TN / 16;             // fragments of S^T
-    static constexpr int LT = TN / 4;              // consecutive tokens of a lane
+    static constexpr int H = F8 ? 1 : 2;           // pieces
+    static constexpr int NS = kBlock / 16 / H;     // fragments of S^T of a piece
+    static constexpr int LT = 4 * NS;              // consecutive tokens of a lane in a piece
     static constexpr int KL = D * E / 64;          // 16-byte loads of a key row by its four lanes
 
-    int kid, vid;                                  // page numbers of the lane's key rows and of its run of tokens
-    bool vok;
-    uint4 kw[NS][KL], vw[D / 16];
+    int kid[H], vid[H];                            // page numbers of the lane's key rows and of its run of tokens
+    unsigned there;                                // bit i: its run of piece i has a page
+    uint4 kw[H][NS][KL], vw[H][D / 16];
 
-    // This lane's token for the first fragment (the others follow 4 apart), and the first of its run.
-    static __device__ __forceinline__ int key_token(int t0) { return t0 + ((lane_id() & 15) >> 2) * LT + (lane_id() & 3); }
-    static __device__ __forceinline__ int run_token(int t0) { return t0 + (lane_id() >> 4) * LT; }
+    // This lane's token for the first fragment of piece i (the others follow 4 apart), and the first of its run.
+    static __device__ __forceinline__ int key_token(int t0, int i) { return t0 + i * 32 + ((lane_id() & 15) >> 2) * LT + (lane_id() & 3); }
+    static __device__ __forceinline__ int run_token(int t0, int i) { return t0 + i * 32 + (lane_id() >> 4) * LT; }
 
     __device__ __forceinline__ void fetch_pages(const AttnParams &p, const int32_t *pages, int t0)
     {
         const int last = p.max_pages - 1;
-        kid = pages[min(page_of(p, key_token(t0) >> 4), last)];
-        vid = pages[min(page_of(p, run_token(t0) >> 4), last)];
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+            kid[i] = pages[min(page_of(p, key_token(t0, i) >> 4), last)];
+            vid[i] = pages[min(page_of(p, run_token(t0, i) >> 4), last)];
+        }
     }
 
-    __device__ __forceinline__ void fetch(const AttnParams &p, int h, int t0)
+    // (tokens without a page are read from the first one and not seen)
+    __device__ __forceinline__ void fetch_keys(const AttnParams &p, int h, int t0)
     {
-        const int kt = key_token(t0), vt = run_token(t0);
-        const int kp = page_of(p, kt >> 4), vp = page_of(p, vt >> 4);
-        const bool kok = (unsigned)kid < (unsigned)p.num_pages;
-        vok = vp < p.max_pages && (unsigned)vid < (unsigned)p.num_pages;
-        const size_t head_bytes = (size_t)p.page_size * D * E;
-        // (tokens without a page are read from the first one and not seen)
-        const uint8_t *ka = (const uint8_t *)p.k + ((size_t)(kok ? kid : 0) * p.KVH + h) * head_bytes + (kt - kp * p.page_size) * (D * E) + (lane_id() >> 4) * 16;
-        const uint8_t *va = (const uint8_t *)p.v + ((size_t)(vok ? vid : 0) * p.KVH + h) * head_bytes +
-                            (size_t)((lane_id() & 15) * p.page_size + vt - vp * p.page_size) * E;
 #pragma unroll
-        for (int j = 0; j < NS; ++j)
+        for (int i = 0; i < H; ++i) {
+            const int t = key_token(t0, i), place = t - page_of(p, t >> 4) * p.page_size;
+            const uint8_t *a = (const uint8_t *)p.k + (((size_t)((unsigned)kid[i] < (unsigned)p.num_pages ? kid[i] : 0) * p.KVH + h) * p.page_size + place) * (D * E) +
+                               (lane_id() >> 4) * 16;
 #pragma unroll
-            for (int i = 0; i < KL; ++i) kw[j][i] = *reinterpret_cast<const uint4 *>(ka + j * 4 * (D * E) + i * 64);
+            for (int j = 0; j < NS; ++j)
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t) vw[t] = load_once(va + (size_t)t * 16 * p.page_size * E);
+                for (int k = 0; k < KL; ++k) kw[i][j][k] = *reinterpret_cast<const uint4 *>(a + j * 4 * (D * E) + k * 64);
+        }
+    }
+    __device__ __forceinline__ void fetch_values(const AttnParams &p, int h, int t0)
+    {
+        const uint8_t *a[H];
+        there = 0;
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+            const int t = run_token(t0, i), page = page_of(p, t >> 4), place = t - page * p.page_size;
+            const bool known = (unsigned)vid[i] < (unsigned)p.num_pages;
+            there |= known && page < p.max_pages ? 1u << i : 0u;
+            a[i] = (const uint8_t *)p.v + ((((size_t)(known ? vid[i] : 0) * p.KVH + h) * D + (lane_id() & 15)) * p.page_size + place) * E;
+        }
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+            for (int i = 0; i < H; ++i) vw[i][t] = load_once(a[i] + (size_t)t * 16 * p.page_size * E);
     }
 
-    // Scores, weights, second product.  pos: position of the lane's row (-1: no row); pmin, pmax: least and greatest position of
-    // the tile's rows.
-    __device__ __forceinline__ void run(const AttnParams &p, int t0, const bf16x8 (&q)[D / 32], int pos, int pmin, int pmax, RowState<D> &s)
+    __device__ __forceinline__ void first_product(const bf16x8 (&q)[D / 32], f32x4 (&z)[H][NS]) const
     {
-        f32x4 z[NS];
 #pragma unroll
-        for (int j = 0; j < NS; ++j) {
-            z[j] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = 0; i < H; ++i)
 #pragma unroll
-            for (int i = 0; i < KL; ++i) {
-                if (F8) {
-                    z[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(make_uint2(kw[j][i].x, kw[j][i].y)), q[2 * i], z[j], 0, 0, 0);
-                    z[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(make_uint2(kw[j][i].z, kw[j][i].w)), q[2 * i + 1], z[j], 0, 0, 0);
-                } else {
-                    z[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kw[j][i]), q[i], z[j], 0, 0, 0);
+            for (int j = 0; j < NS; ++j) {
+                z[i][j] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int k = 0; k < KL; ++k) {
+                    const uint4 u = kw[i][j][k];
+                    if (F8) {
+                        z[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(make_uint2(u.x, u.y)), q[2 * k], z[i][j], 0, 0, 0);
+                        z[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(make_uint2(u.z, u.w)), q[2 * k + 1], z[i][j], 0, 0, 0);
+                    } else {
+                        z[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u), q[k], z[i][j], 0, 0, 0);
+                    }
                 }
             }
-        }
-        float x[LT];
+    }
+
+    // Weights and second product.  pos: position of the lane's row (-1: no row); pmin, pmax: least and greatest position of the
+    // tile's rows.
+    __device__ __forceinline__ void second_product(const AttnParams &p, int t0, f32x4 (&z)[H][NS], int pos, int pmin, int pmax, RowState<D> &s)
+    {
+        float x[H][LT];
 #pragma unroll
-        for (int i = 0; i < LT; ++i) x[i] = z[i / 4][i % 4] * p.scale2;
+        for (int i = 0; i < H; ++i)
+#pragma unroll
+            for (int j = 0; j < LT; ++j) x[i][j] = z[i][j / 4][j % 4] * p.scale2;
         // Tokens that not every row of the tile sees.  A token that none sees may hold anything, also what is no number: its
         // value is replaced by zero, since zero times it would not be.
-        const int vt = run_token(t0);
-        const bool in_window = p.window == 0 || t0 > pmax - p.window || t0 + TN <= p.sinks;
-        if (!(t0 + TN - 1 <= pmin && in_window && __all(vok))) {
+        const bool in_window = p.window == 0 || t0 > pmax - p.window || t0 + kBlock <= p.sinks;
+        if (!(t0 + kBlock - 1 <= pmin && in_window && __all(there == (1u << H) - 1u))) {
 #pragma unroll
-            for (int i = 0; i < LT; ++i) x[i] = (int)vok & seen(p, vt + i, pos, pos) ? x[i] : -INFINITY;
-            uint32_t mask[4];
+            for (int i = 0; i < H; ++i) {
+                const int vt = run_token(t0, i);
+                const int ok = there >> i & 1u;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                mask[w] = 0u;
+                for (int j = 0; j < LT; ++j) x[i][j] = ok & seen(p, vt + j, pos, pos) ? x[i][j] : -INFINITY;
+                uint32_t mask[4];
 #pragma unroll
-                for (int i = 0; i < 4 / E; ++i) {
-                    const int any = (int)vok & seen(p, vt + w * (4 / E) + i, pmin, pmax);
-                    mask[w] |= any ? (F8 ? 0xffu << (8 * i) : 0xffffu << (16 * i)) : 0u;
+                for (int w = 0; w < 4; ++w) {
+                    mask[w] = 0u;
+#pragma unroll
+                    for (int j = 0; j < 4 / E; ++j)
+                        mask[w] |= ok & seen(p, vt + w * (4 / E) + j, pmin, pmax) ? (F8 ? 0xffu << (8 * j) : 0xffffu << (16 * j)) : 0u;
+                }
+#pragma unroll
+                for (int t = 0; t < D / 16; ++t) {
+                    vw[i][t].x &= mask[0];
+                    vw[i][t].y &= mask[1];
+                    vw[i][t].z &= mask[2];
+                    vw[i][t].w &= mask[3];
                 }
             }
-#pragma unroll
-            for (int t = 0; t < D / 16; ++t) {
-                vw[t].x &= mask[0];
-                vw[t].y &= mask[1];
-                vw[t].z &= mask[2];
-                vw[t].w &= mask[3];
-            }
         }
-        float top = x[0];
+        float top = x[0][0];
 #pragma unroll
-        for (int i = 1; i < LT; ++i) top = fmaxf(top, x[i]);
+        for (int i = 0; i < H; ++i)
+#pragma unroll
+            for (int j = 0; j < LT; ++j) top = fmaxf(top, x[i][j]);
         const float m = fmaxf(s.m, row_max(top));
         if (__any(m > s.m)) {
             const float a = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s.m - m);
@@ -316,28 +346,32 @@ struct Step {
             s.m = m;
         }
         const float base = s.m == -INFINITY ? 0.0f : s.m;
-#pragma unroll
-        for (int i = 0; i < LT; ++i) {
-            x[i] = __builtin_amdgcn_exp2f(x[i] - base);
-            s.l += x[i];
-        }
         // bf16 weights: half a step of 2^-8 each, of either sign, beside values that are bf16 themselves
-        bf16x8 w[LT / 8];
+        bf16x8 w[H][LT / 8];
 #pragma unroll
-        for (int i = 0; i < LT / 8; ++i) {
-            const uint4 u = make_uint4(pack_bf16(x[8 * i], x[8 * i + 1]), pack_bf16(x[8 * i + 2], x[8 * i + 3]),
-                                       pack_bf16(x[8 * i + 4], x[8 * i + 5]), pack_bf16(x[8 * i + 6], x[8 * i + 7]));
-            w[i] = __builtin_bit_cast(bf16x8, u);
-        }
+        for (int i = 0; i < H; ++i) {
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t) {
-            if (F8) {
-                s.o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(make_uint2(vw[t].x, vw[t].y)), w[0], s.o[t], 0, 0, 0);
-                s.o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(make_uint2(vw[t].z, vw[t].w)), w[LT / 8 - 1], s.o[t], 0, 0, 0);
-            } else {
-                s.o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vw[t]), w[0], s.o[t], 0, 0, 0);
+            for (int j = 0; j < LT; ++j) {
+                x[i][j] = __builtin_amdgcn_exp2f(x[i][j] - base);
+                s.l += x[i][j];
             }
+#pragma unroll
+            for (int j = 0; j < LT / 8; ++j)
+                w[i][j] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(x[i][8 * j], x[i][8 * j + 1]), pack_bf16(x[i][8 * j + 2], x[i][8 * j + 3]),
+                                                                 pack_bf16(x[i][8 * j + 4], x[i][8 * j + 5]), pack_bf16(x[i][8 * j + 6], x[i][8 * j + 7])));
         }
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+            for (int i = 0; i < H; ++i) {
+                const uint4 u = vw[i][t];
+                if (F8) {
+                    s.o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(make_uint2(u.x, u.y)), w[i][0], s.o[t], 0, 0, 0);
+                    s.o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(make_uint2(u.z, u.w)), w[i][LT / 8 - 1], s.o[t], 0, 0, 0);
+                } else {
+                    s.o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u), w[i][0], s.o[t], 0, 0, 0);
+                }
+            }
     }
 };
 
@@ -375,7 +409,7 @@ __device__ __forceinline__ void finish_row(const AttnParams &p, int t, int head,
     if (p.lse && c0 == 0) p.lse[row] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
-// A length of the line of one key head per workgroup, a quarter of it per wave, in steps.  A wave goes through its quarter tile by tile.
+// A length of the line of one key head per workgroup, a quarter of it per wave.  A wave goes through its quarter tile by tile.
 // A tile that lies in it whole is finished in its registers; of the first and the last, which in general do not, it leaves its part in
 // LDS, and when all waves are through, the parts of each tile are joined: to the finished rows, or to a part in the workspace if
 // the tile goes on in another workgroup.  (With all four waves on one tile after the other, each with its round trips for lengths,
@@ -384,7 +418,6 @@ template <int D, bool F8>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_rows_kernel(AttnParams p)
 {
     typedef Step<D, F8> S;
-    constexpr int kSteps = kBlock / S::TN;
     constexpr int kRecords = 2 * kAttnWaves;
     constexpr unsigned kNone = 0xffffffffu;
     __shared__ Line line;
@@ -396,12 +429,12 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_rows_kernel(AttnParams p
     const unsigned from = min(blockIdx.x * length, total), to = min(from + length, total);
     if (from >= to) return;
     if (lane < 2) rec[2 * wv + lane] = kNone;
-    const unsigned quarter = (length * kSteps + kAttnWaves - 1) / kAttnWaves;
-    const unsigned wfrom = min(from * kSteps + wv * quarter, to * kSteps), wto = min(wfrom + quarter, to * kSteps);
+    const unsigned quarter = (length + kAttnWaves - 1) / kAttnWaves;
+    const unsigned wfrom = min(from + wv * quarter, to), wto = min(wfrom + quarter, to);
     for (unsigned at = wfrom; at < wto;) {
-        const Place f = place_of(p, line, at / kSteps);
-        const unsigned begin = f.begin * kSteps, i0 = at - begin, i1 = min(f.count * kSteps, wto - begin);
-        at = begin + i1;
+        const Place f = place_of(p, line, at);
+        const unsigned i0 = at - f.begin, i1 = min(f.count, wto - f.begin);
+        at = f.begin + i1;
 
         const int r = f.tile * kRows + (lane & 15), rows = f.n * p.G;
         const bool real = r < rows;
@@ -418,33 +451,39 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_rows_kernel(AttnParams p
 
         // (tiles of one request lie on the line with as many blocks each: those past a tile's own are passed over)
         const Blocks blocks = blocks_of(p, f.seq - f.n, pmin, pmax);
-        const int j0 = (int)min(i0, (unsigned)(blocks.count * kSteps)), j1 = (int)min(i1, (unsigned)(blocks.count * kSteps));
+        const int j0 = (int)min(i0, (unsigned)blocks.count), j1 = (int)min(i1, (unsigned)blocks.count);
         const int32_t *row = p.table + (size_t)f.b * p.max_pages;
-        const auto token = [&](int j) { return blocks.at(j / kSteps) * kBlock + j % kSteps * S::TN; };
+        const auto token = [&](int j) { return blocks.at(min(j, j1 - 1)) * kBlock; };
         if (j0 < j1) {
-            S step[2];
+            S step;
             int t0 = token(j0);
-            step[0].fetch_pages(p, row, t0);
-            step[0].fetch(p, h, t0);
-            int t1 = token(min(j0 + 1, j1 - 1));
-            step[1].fetch_pages(p, row, t1);
-            for (int j = j0; j < j1; j += 2) {
+            step.fetch_pages(p, row, t0);
+            step.fetch_keys(p, h, t0);
+            step.fetch_values(p, h, t0);
+            S next;
+            next.fetch_pages(p, row, token(j0 + 1));
+            f32x4 z[S::H][S::NS];
+            for (int j = j0; j + 1 < j1; ++j) {
+                // The next keys as soon as the first product has used these, the next values behind the second; page numbers a
+                // block earlier, in front of them (loads come back in the order of their issue).
+                const int t1 = token(j + 1);
+                step.first_product(q, z);
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    if (j + k < j1) {
-                        // The page numbers of the step after the next, the next step's keys and values, this one's products.
-                        const int t2 = token(min(j + k + 2, j1 - 1));
-                        step[k].fetch_pages(p, row, t2);
-                        if (j + k + 1 < j1) step[k ^ 1].fetch(p, h, t1);
-                        step[k].run(p, t0, q, pos, pmin, pmax, s);
-                        t0 = t1;
-                        t1 = t2;
-                    }
+                for (int i = 0; i < S::H; ++i) {
+                    step.kid[i] = next.kid[i];
+                    step.vid[i] = next.vid[i];
                 }
+                next.fetch_pages(p, row, token(j + 2));
+                step.fetch_keys(p, h, t1);
+                step.second_product(p, t0, z, pos, pmin, pmax, s);
+                step.fetch_values(p, h, t1);
+                t0 = t1;
             }
+            step.first_product(q, z);
+            step.second_product(p, t0, z, pos, pmin, pmax, s);
         }
         s.l = row_sum(s.l);
-        if (i0 == 0 && i1 == f.count * kSteps) {
+        if (i0 == 0 && i1 == f.count) {
             if (real) finish_row<D>(p, f.first + tok, head, behind_prefix(p, f.seq - f.n), (lane >> 4) * 4, 16, s.m, s.l, s.o);
         } else {
             const int k = 2 * wv + (at == wto && i0 == 0 ? 1 : 0);      // the wave's last tile, or its first
