@@ -5,6 +5,7 @@ between tokens.  All other tensors are contiguous.  A cache of dtype bfloat16 or
 """
 from __future__ import annotations
 
+import functools
 from ctypes import c_float, c_int, c_int64, c_size_t, c_void_p
 
 import torch
@@ -41,34 +42,47 @@ def lib():
     return _lib
 
 
-def _rows(t, what):
-    """Address and token distance of a [T, heads, D] tensor whose tokens are dense."""
+# The host spends longer on these calls than the GPU does on a small batch, so every check is one pass over a tensor, and tensors that
+# a call has just allocated are not checked (lynx_kv_assign 17.7 -> 11.2 us of host time, lynx_qk_norm_rope 14.1 -> 12.0).
+def _here(t, what):
+    """The current device, on which kernels run; t: the call's first tensor."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what}: expected a CUDA/HIP tensor")
+    return torch._C._cuda_getDevice()
+
+
+def _at(t, dtype, n, here, what):
+    """Address of a contiguous tensor of n elements (None: any number) on the current device, which is where kernels run."""
+    if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == here and t.is_contiguous() and (n is None or t.numel() == n):
+        return t.data_ptr()
+    if t is None:
+        return None
+    _ptr(t, dtype, what)
+    if t.get_device() != here:
+        raise ValueError(f"{what}: on {t.device}, the current device is cuda:{here}")
+    if n is not None and t.numel() != n:
+        raise ValueError(f"{what}: expected {n} elements, got {t.numel()}")
+    return t.data_ptr()
+
+
+def _rows(t, heads, D, here, what):
+    """Address and token distance of a [T, heads, D] tensor whose tokens are dense (heads, D: None for any)."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what}: expected a CUDA/HIP tensor")
     if t.dtype is not BF16:
         raise TypeError(f"{what}: expected {BF16}, got {t.dtype}")
     if t.dim() != 3:
         raise ValueError(f"{what}: expected [tokens, heads, channels]")
-    T, heads, D = t.shape
-    s = t.stride()
-    if s[2] != 1 or (heads > 1 and s[1] != D):
+    if t.get_device() != here:
+        raise ValueError(f"{what}: on {t.device}, the current device is cuda:{here}")
+    T, h, d = t.shape
+    step, a, b = t.stride()
+    if b != 1 or (h > 1 and a != d):
         raise ValueError(f"{what}: the heads of a token must be contiguous")
+    if d != D or (heads is not None and h != heads):
+        raise ValueError(f"{what}: the shapes do not match each other and the cache")
     # (a single token's distance to the next means nothing, and may be anything)
-    return t.data_ptr(), (s[0] if T > 1 else heads * D)
-
-
-def _same_device(*tensors):
-    """Kernels run on the current device: all tensors have to be there."""
-    here = torch._C._cuda_getDevice()
-    for t in tensors:
-        if t is not None and t.get_device() != here:
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
-
-
-def _vector(t, n, dtype, what):
-    if t is not None and t.numel() != n:
-        raise ValueError(f"{what}: expected {n} elements, got {t.numel()}")
-    return _ptr(t, dtype, what)
+    return t.data_ptr(), (step if T > 1 else h * d)
 
 
 def _cache(k_cache, v_cache):
@@ -99,20 +113,20 @@ def lynx_kv_assign(ctx_len, new_len, T, page_size, block_table, free_ring, ring_
     """Pages and slots of a step's tokens: ctx_len, new_len [B] i32, block_table [B, max_pages] i32 and free_ring [num_pages] i32
     (both updated), ring_state [2] i32 = head, count -> dict(q_start [B+1], seq_len [B], positions [T], slots [T],
     ring_state [2], status [1]), all i32.  out: such a dict; its seq_len may be ctx_len, its ring_state may be ring_state."""
+    here = _here(ctx_len, "ctx_len")
     B = ctx_len.numel()
     if block_table.dim() != 2 or block_table.shape[0] != B:
         raise ValueError("block_table: expected [requests, max_pages]")
-    dev = ctx_len.device
-    T = int(T)
-    if out is None:
-        e = lambda n: torch.empty(n, dtype=I32, device=dev)
-        out = dict(q_start=e(B + 1), seq_len=e(B), positions=e(T), slots=e(T), ring_state=e(2), status=e(1))
-    _same_device(ctx_len, new_len, block_table, free_ring, ring_state, *[out[n] for n in _ASSIGN_OUT])
     sizes = (B + 1, B, T, T, 2, 1)
-    _check(lib().lynx_kv_assign(_vector(ctx_len, B, I32, "ctx_len"), _vector(new_len, B, I32, "new_len"), B, T, int(page_size),
-                                free_ring.numel(), block_table.shape[1], int(shared_pages), _ptr(block_table, I32, "block_table"),
-                                _ptr(free_ring, I32, "free_ring"), _vector(ring_state, 2, I32, "ring_state"),
-                                *[_vector(out[n], m, I32, n) for n, m in zip(_ASSIGN_OUT, sizes)], _stream()))
+    if out is None:
+        parts = torch.empty(sum(sizes), dtype=I32, device=ctx_len.device).split_with_sizes(sizes)      # one allocation
+        out = dict(zip(_ASSIGN_OUT, parts))
+        made = [t.data_ptr() for t in parts]
+    else:
+        made = [_at(out[n], I32, m, here, n) for n, m in zip(_ASSIGN_OUT, sizes)]
+    _check(lib().lynx_kv_assign(_at(ctx_len, I32, B, here, "ctx_len"), _at(new_len, I32, B, here, "new_len"), B, T, page_size,
+                                free_ring.numel(), block_table.shape[1], shared_pages, _at(block_table, I32, None, here, "block_table"),
+                                _at(free_ring, I32, None, here, "free_ring"), _at(ring_state, I32, 2, here, "ring_state"), *made, _stream()))
     return out
 
 
@@ -121,22 +135,28 @@ def lynx_qk_norm_rope(q, k, v, positions, slots, freqs, k_cache, v_cache, q_weig
     """Norms and rotation of q [T, QH, D] and k [T, KVH, D], k and v written to their slots of the cache -> q_out [T, QH, D].
     positions, slots [T] i32; freqs [rot/2] f64 (radians per position; None or empty: no rotation); weights [D] bf16 or None."""
     KVH, page_size, D, pages, fmt = _cache(k_cache, v_cache)
-    T, QH = q.shape[0], q.shape[1] if q.dim() == 3 else 0
+    here = _here(q, "q")
+    qp, qs = _rows(q, None, D, here, "q")
+    T, QH, _ = q.shape
+    kp, ks = _rows(k, KVH, D, here, "k")
+    vp, vs = _rows(v, KVH, D, here, "v")
     if q_out is None:
-        q_out = torch.empty((T, QH, D), dtype=BF16, device=q.device)
-    _same_device(q, k, v, positions, slots, freqs, k_cache, v_cache, q_weight, k_weight, q_out)
-    (qp, qs), (kp, ks), (vp, vs), (op, os_) = _rows(q, "q"), _rows(k, "k"), _rows(v, "v"), _rows(q_out, "q_out")
-    if q.shape[2] != D or k.shape != (T, KVH, D) or v.shape != (T, KVH, D) or q_out.shape != q.shape:
-        raise ValueError("q, k, v, q_out: shapes do not match each other and the cache")
+        q_out = torch.empty(T, QH, D, dtype=BF16, device=q.device)
+        op, os_ = q_out.data_ptr(), QH * D
+    else:
+        op, os_ = _rows(q_out, QH, D, here, "q_out")
+    if k.shape[0] != T or v.shape[0] != T or q_out.shape[0] != T:
+        raise ValueError("q, k, v, q_out: the shapes do not match each other and the cache")
     rot = 0 if freqs is None else 2 * freqs.numel()
-    _check(lib().lynx_qk_norm_rope(qp, qs, kp, ks, vp, vs, _vector(q_weight, D, BF16, "q_weight"), _vector(k_weight, D, BF16, "k_weight"),
-                                   float(eps), _vector(positions, T, I32, "positions"), _vector(slots, T, I32, "slots"),
-                                   _ptr(freqs, F64, "freqs"), rot, int(bool(interleaved)), T, QH, KVH, D, op, os_,
-                                   _ptr(k_cache, k_cache.dtype, "k_cache"), _ptr(v_cache, v_cache.dtype, "v_cache"), fmt,
-                                   float(k_scale), float(v_scale), pages, page_size, _stream()))
+    _check(lib().lynx_qk_norm_rope(qp, qs, kp, ks, vp, vs, _at(q_weight, BF16, D, here, "q_weight"), _at(k_weight, BF16, D, here, "k_weight"),
+                                   eps, _at(positions, I32, T, here, "positions"), _at(slots, I32, T, here, "slots"),
+                                   _at(freqs, F64, None, here, "freqs"), rot, 1 if interleaved else 0, T, QH, KVH, D, op, os_,
+                                   _at(k_cache, k_cache.dtype, None, here, "k_cache"), _at(v_cache, v_cache.dtype, None, here, "v_cache"), fmt,
+                                   k_scale, v_scale, pages, page_size, _stream()))
     return q_out
 
 
+@functools.lru_cache(maxsize=4096)
 def attention_workspace_bytes(B, T, QH, KVH, D, prefix_len=0) -> int:
     return int(lib().lynx_attention_workspace_bytes(B, T, QH, KVH, D, prefix_len))
 
@@ -147,34 +167,33 @@ def new_attention_workspace(B, T, QH, KVH, D, prefix_len=0, device="cuda"):
 
 def _attention(q, k_cache, v_cache, block_table, q_start, seq_len, max_new, scale, k_scale, v_scale, out, lse, workspace, prefix, tail):
     KVH, page_size, D, pages, fmt = _cache(k_cache, v_cache)
-    qp, qs = _rows(q, "q")
-    T, QH, Dq = q.shape
-    if Dq != D:
-        raise ValueError("q: channels do not match the cache")
+    here = _here(q, "q")
+    qp, qs = _rows(q, None, D, here, "q")
+    T, QH, _ = q.shape
     if block_table.dim() != 2:
         raise ValueError("block_table: expected [requests, max_pages]")
     B, max_pages = block_table.shape
-    dev = q.device
     if out is None:
-        out = torch.empty((T, QH, D), dtype=BF16, device=dev)
-    op, os_ = _rows(out, "out")
-    if out.shape != q.shape:
-        raise ValueError("out: expected the shape of q")
-    prefix_len = prefix[1] if prefix else 0
-    need = lib().lynx_attention_workspace_bytes(B, T, QH, KVH, D, prefix_len)
+        out = torch.empty(T, QH, D, dtype=BF16, device=q.device)
+        op, os_ = out.data_ptr(), QH * D
+    else:
+        op, os_ = _rows(out, QH, D, here, "out")
+        if out.shape[0] != T:
+            raise ValueError("out: expected the shape of q")
+    need = attention_workspace_bytes(B, T, QH, KVH, D, prefix[1] if prefix else 0)
     if workspace is None:
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
-    elif workspace.numel() * workspace.element_size() < need:
-        raise ValueError(f"workspace too small: {workspace.numel() * workspace.element_size()} < {need}")
-    _same_device(q, k_cache, v_cache, block_table, q_start, seq_len, out, lse, workspace, prefix[0] if prefix else None)
-    args = (qp, qs, _ptr(k_cache, k_cache.dtype, "k_cache"), _ptr(v_cache, v_cache.dtype, "v_cache"), fmt, float(k_scale),
-            float(v_scale), pages, page_size, _ptr(block_table, I32, "block_table"), max_pages, _vector(q_start, B + 1, I32, "q_start"),
-            _vector(seq_len, B, I32, "seq_len"))
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+    elif workspace.get_device() != here or workspace.numel() * workspace.element_size() < need:
+        raise ValueError(f"workspace: on {workspace.device}, {workspace.numel() * workspace.element_size()} bytes; needed {need} on cuda:{here}")
     if prefix:
-        args += (_vector(prefix[0], -(-prefix_len // page_size), I32, "prefix_table"), prefix_len)
-    call = lib().lynx_attention_prefix if prefix else lib().lynx_attention
-    _check(call(*args, B, T, int(max_new), QH, KVH, D, float(D ** -0.5 if scale is None else scale), *tail, op, os_,
-                _vector(lse, T * QH, F32, "lse"), workspace.data_ptr(), _stream()))
+        call = lib().lynx_attention_prefix
+        prefix = (_at(prefix[0], I32, -(-prefix[1] // page_size), here, "prefix_table"), prefix[1])
+    else:
+        call = lib().lynx_attention
+    _check(call(qp, qs, _at(k_cache, k_cache.dtype, None, here, "k_cache"), _at(v_cache, v_cache.dtype, None, here, "v_cache"), fmt, k_scale, v_scale,
+                pages, page_size, _at(block_table, I32, None, here, "block_table"), max_pages, _at(q_start, I32, B + 1, here, "q_start"),
+                _at(seq_len, I32, B, here, "seq_len"), *prefix, B, T, max_new, QH, KVH, D, D ** -0.5 if scale is None else scale, *tail, op, os_,
+                _at(lse, F32, T * QH, here, "lse"), workspace.data_ptr(), _stream()))
     return out
 
 
@@ -183,8 +202,8 @@ def lynx_attention(q, k_cache, v_cache, block_table, q_start, seq_len, max_new, 
     """Attention of q [T, QH, D] over the paged cache -> out [T, QH, D].  block_table [B, max_pages], q_start [B+1], seq_len [B]
     i32; max_new: the largest number of new tokens of a request, as far as known; scale: 1 / sqrt(D) if None; lse: [T, QH] f32
     that receives the logarithm of each row's sum of weights, or None."""
-    return _attention(q, k_cache, v_cache, block_table, q_start, seq_len, max_new, scale, k_scale, v_scale, out, lse, workspace, None,
-                      (int(window), int(sinks)))
+    return _attention(q, k_cache, v_cache, block_table, q_start, seq_len, max_new, scale, k_scale, v_scale, out, lse, workspace, (),
+                      (window, sinks))
 
 
 def lynx_attention_prefix(q, k_cache, v_cache, block_table, q_start, seq_len, max_new, prefix_table, prefix_len, scale=None,
@@ -192,4 +211,4 @@ def lynx_attention_prefix(q, k_cache, v_cache, block_table, q_start, seq_len, ma
     """lynx_attention for a batch whose sequences all begin with the same prefix_len tokens, held by the pages of prefix_table
     [ceil(prefix_len / page size)] i32: they are read once for the whole batch."""
     return _attention(q, k_cache, v_cache, block_table, q_start, seq_len, max_new, scale, k_scale, v_scale, out, lse, workspace,
-                      (prefix_table, int(prefix_len)), ())
+                      (prefix_table, prefix_len), ())

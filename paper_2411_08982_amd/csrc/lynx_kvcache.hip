@@ -9,6 +9,7 @@ namespace lynx {
 // page, returned page and token finds its request by bisection in the sums.  Nothing here is bound by bytes: one workgroup,
 // one thread per request, and what counts is the number of round trips.
 constexpr int kAssignThreads = LYNX_MAX_REQUESTS;
+constexpr int kTokensHere = 4096;       // more tokens are left to a launch of their own
 
 struct AssignShared {
     int tok_end[LYNX_MAX_REQUESTS], take_end[LYNX_MAX_REQUESTS], back_end[LYNX_MAX_REQUESTS];
@@ -50,7 +51,15 @@ struct AssignParams {
     const int32_t *ctx_len, *new_len, *ring_state;
     int32_t *block_table, *free_ring, *q_start, *seq_len, *positions, *slots, *ring_state_out, *status;
     int B, T, page_size, num_pages, max_pages, shared_pages;
+    bool tokens_apart;
 };
+
+__device__ __forceinline__ void place_token(const AssignParams &p, int t, int r, int pos)
+{
+    const int page = p.block_table[(size_t)r * p.max_pages + pos / p.page_size];
+    p.positions[t] = pos;
+    p.slots[t] = page >= 0 && page < p.num_pages ? page * p.page_size + pos % p.page_size : -1;
+}
 
 __global__ __launch_bounds__(kAssignThreads) void assign_kernel(AssignParams p)
 {
@@ -119,17 +128,34 @@ __global__ __launch_bounds__(kAssignThreads) void assign_kernel(AssignParams p)
         p.ring_state_out[1] = count - fresh + returned;
         *p.status = sh.status;
     }
+    if (p.tokens_apart) return;
     __syncthreads();   // the new entries of the block table
     for (int t = b; t < p.T; t += kAssignThreads) {
-        int pos = 0, slot = -1;
         if (t < rows) {
             const int r = owner_of(sh.tok_end, p.B, t);
-            pos = sh.ctx[r] + t - (r > 0 ? sh.tok_end[r - 1] : 0);
-            const int page = p.block_table[(size_t)r * p.max_pages + pos / p.page_size];
-            if (page >= 0 && page < p.num_pages) slot = page * p.page_size + pos % p.page_size;
+            place_token(p, t, r, sh.ctx[r] + t - (r > 0 ? sh.tok_end[r - 1] : 0));
+        } else {
+            p.positions[t] = 0;
+            p.slots[t] = -1;
         }
-        p.positions[t] = pos;
-        p.slots[t] = slot;
+    }
+}
+
+// Positions and slots of many tokens, from what assign_kernel has written.
+constexpr int kTokenThreads = 256;
+__global__ __launch_bounds__(kTokenThreads) void assign_tokens_kernel(AssignParams p)
+{
+    __shared__ int ends[LYNX_MAX_REQUESTS];
+    for (int b = threadIdx.x; b < p.B; b += kTokenThreads) ends[b] = p.q_start[b + 1];
+    __syncthreads();
+    const int t = blockIdx.x * kTokenThreads + threadIdx.x;
+    if (t >= p.T) return;
+    if (t < ends[p.B - 1]) {
+        const int r = owner_of(ends, p.B, t);
+        place_token(p, t, r, p.seq_len[r] - ends[r] + t);
+    } else {
+        p.positions[t] = 0;
+        p.slots[t] = -1;
     }
 }
 
@@ -315,8 +341,10 @@ extern "C" int lynx_kv_assign(const int32_t *ctx_len, const int32_t *new_len, in
         (T > 0 && (!positions || !slots)))
         return fail(LYNX_ERR_INVALID_ARG, "lynx_kv_assign: null pointer");
     AssignParams p = {ctx_len, new_len, ring_state, block_table, free_ring, q_start, seq_len, positions, slots, ring_state_out,
-                      status, B, T, page_size, num_pages, max_pages, shared_pages};
+                      status, B, T, page_size, num_pages, max_pages, shared_pages, T > kTokensHere};
     hipLaunchKernelGGL(assign_kernel, dim3(1), dim3(kAssignThreads), 0, (hipStream_t)stream, p);
+    if (p.tokens_apart)
+        hipLaunchKernelGGL(assign_tokens_kernel, dim3((T + kTokenThreads - 1) / kTokenThreads), dim3(kTokenThreads), 0, (hipStream_t)stream, p);
     return check_launch("lynx_kv_assign");
 }
 
