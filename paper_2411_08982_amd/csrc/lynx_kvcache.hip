@@ -160,9 +160,13 @@ __global__ __launch_bounds__(kTokenThreads) void assign_tokens_kernel(AssignPara
 }
 
 // ---- lynx_qk_norm_rope ------------------------------------------------------------------------------------------------
-// One workgroup per token.  The angles of a token are the same for all its heads: they are computed once, into LDS.  A head row
-// is held by D/8 lanes, 8 channels (16 bytes) each.
+// Workgroups of two kinds in one launch.  The first T have a token each, for its queries and keys: the angles are the same for all
+// heads and computed once, into LDS; a head row is held by D/8 lanes, 8 channels (16 bytes) each.  The others turn 64 tokens' values
+// of one key head over in LDS, since the cache has them transposed: where the tokens' slots follow one another, as a prompt's do, a
+// channel's run of 16 bytes is one store.  (Element by element 8001 tokens with 8 key heads took 70 us, with 16 of 16 heads 141.)
 constexpr int kRopeThreads = 256;
+constexpr int kTurnTokens = 64;
+constexpr int kFewTokens = 1024;        // up to so many tokens 16 at a time, for more workgroups
 
 struct RopeParams {
     const uint16_t *q, *k, *v, *q_weight, *k_weight;
@@ -172,7 +176,8 @@ struct RopeParams {
     uint16_t *q_out;
     void *k_cache, *v_cache;
     float eps, k_scale, v_scale;
-    int rot, interleaved, QH, KVH, num_slots, page_size;
+    int rot, interleaved, T, QH, KVH, num_slots, page_size;
+    int turn;                   // tokens of a workgroup for values: kTurnTokens or fewer
 };
 
 __device__ __forceinline__ void unpack8(uint4 u, float (&x)[8])
@@ -205,13 +210,101 @@ __device__ __forceinline__ uint2 pack8_fp8(const float (&x)[8], float scale)
     return make_uint2((unsigned)a, (unsigned)b);
 }
 
+// The values of up to 64 tokens of one key head into the cache.
+template <int D, bool F8>
+__device__ __forceinline__ void write_values(const RopeParams &p, int t0, int h, uint8_t *lds, uint8_t (&list)[2][kTurnTokens])
+{
+    constexpr int E = F8 ? 1 : 2;
+    constexpr int RUN = 16 / E;                                  // tokens of a 16-byte run
+    constexpr int kStride = kTurnTokens * E + 8;                 // bytes of a channel in LDS
+    const int tid = threadIdx.x, lane = lane_id();
+    // every wave for itself: lane i looks at token t0 + i
+    const int slot = lane < p.turn && t0 + lane < p.T ? p.slots[t0 + lane] : -1;
+    const bool valid = slot >= 0 && slot < p.num_slots;
+    const int next = __shfl(slot, lane + 1);
+    const unsigned long long follow = __ballot(valid && lane < kWave - 1 && next == slot + 1 && next < p.num_slots);
+    // runs that begin at a token: its slot begins a run of the cache, and the next RUN - 1 tokens' follow
+    const unsigned long long runs = __ballot(valid && slot % RUN == 0 && lane <= kTurnTokens - RUN && (follow >> lane & ((1ull << (RUN - 1)) - 1)) == (1ull << (RUN - 1)) - 1);
+    unsigned long long covered = runs;
+#pragma unroll
+    for (int i = 1; i < RUN; i *= 2) covered |= covered << i;
+    const unsigned long long single = __ballot(valid) & ~covered;
+    // the tokens that begin runs, and those in none
+    const unsigned long long before = (1ull << lane) - 1;
+    if (tid < kWave) {
+        if (runs >> lane & 1) list[0][__popcll(runs & before)] = (uint8_t)lane;
+        if (single >> lane & 1) list[1][__popcll(single & before)] = (uint8_t)lane;
+    }
+    for (int i = tid; i < p.turn * (D / 8); i += kRopeThreads) {
+        const int tok = i / (D / 8), c = i % (D / 8) * 8;
+        if (t0 + tok >= p.T) break;
+        const uint4 u = *reinterpret_cast<const uint4 *>(p.v + (size_t)(t0 + tok) * p.v_stride + (size_t)h * D + c);
+        if (F8) {
+            float x[8];
+            unpack8(u, x);
+            const uint2 w = pack8_fp8(x, p.v_scale);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) lds[(c + j) * kStride + tok] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+        } else {
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) *reinterpret_cast<uint16_t *>(lds + (c + j) * kStride + tok * 2) = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+        }
+    }
+    __syncthreads();
+    const int n = __popcll(runs);
+    uint8_t *const cache = (uint8_t *)p.v_cache;
+    const auto place = [&](int s, int d) {
+        const int page = s / p.page_size;
+        return cache + ((((size_t)page * p.KVH + h) * D + d) * p.page_size + (s - page * p.page_size)) * E;
+    };
+    // a channel's runs beside one another: they lie beside one another in the page
+    for (int i = tid; i < n * D; i += kRopeThreads) {
+        const int d = i / n, tok = list[0][i - d * n];
+        const uint2 *src = reinterpret_cast<const uint2 *>(lds + d * kStride + tok * E);
+        uint4 u;
+        if (tok * E % 8 == 0) {
+            const uint2 lo = src[0], hi = src[1];
+            u = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        } else {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                w[j] = 0;
+#pragma unroll
+                for (int e = 0; e < 4 / E; ++e) {
+                    const uint8_t *q = lds + d * kStride + tok * E + j * 4 + e * E;
+                    w[j] |= F8 ? (uint32_t)*q << (8 * e) : (uint32_t) * reinterpret_cast<const uint16_t *>(q) << (16 * e);
+                }
+            }
+            u = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        *reinterpret_cast<uint4 *>(place(p.slots[t0 + tok], d)) = u;
+    }
+    const int ns = __popcll(single);
+    for (int i = tid; i < ns * D; i += kRopeThreads) {
+        const int tok = list[1][i / D], d = i % D;
+        uint8_t *dst = place(p.slots[t0 + tok], d);
+        if (F8) *dst = lds[d * kStride + tok];
+        else *reinterpret_cast<uint16_t *>(dst) = *reinterpret_cast<const uint16_t *>(lds + d * kStride + tok * 2);
+    }
+}
+
 template <int D, bool F8>
 __global__ __launch_bounds__(kRopeThreads) void norm_rope_kernel(RopeParams p)
 {
     constexpr int L = D / 8;                    // lanes of a row
     constexpr int R = kRopeThreads / L;         // rows of a pass
-    __shared__ float sc[D / 2], ss[D / 2];
-    const int t = blockIdx.x, tid = threadIdx.x;
+    __shared__ __align__(16) uint8_t turned[D * (kTurnTokens * (F8 ? 1 : 2) + 8)];
+    __shared__ uint8_t list[2][kTurnTokens];
+    float *const sc = reinterpret_cast<float *>(turned), *const ss = sc + D / 2;
+    const int tid = threadIdx.x;
+    if ((int)blockIdx.x >= p.T) {
+        const int i = blockIdx.x - p.T;
+        write_values<D, F8>(p, i / p.KVH * p.turn, i % p.KVH, turned, list);
+        return;
+    }
+    const int t = blockIdx.x;
     const int half = p.rot / 2;
     if (tid < half) {
         // turns, reduced to [-1/2, 1/2] in 64 bits
@@ -226,13 +319,13 @@ __global__ __launch_bounds__(kRopeThreads) void norm_rope_kernel(RopeParams p)
     const bool keep = slot >= 0 && slot < p.num_slots;
     const int page = keep ? slot / p.page_size : 0, place = keep ? slot % p.page_size : 0;
     const int c0 = (tid % L) * 8;
-    for (int row = tid / L; row < p.QH + 2 * p.KVH; row += R) {
-        const bool is_q = row < p.QH, is_v = row >= p.QH + p.KVH;
-        const int h = is_q ? row : is_v ? row - p.QH - p.KVH : row - p.QH;
-        const uint16_t *src = is_q ? p.q + t * p.q_stride : is_v ? p.v + t * p.v_stride : p.k + t * p.k_stride;
+    for (int row = tid / L; row < p.QH + p.KVH; row += R) {
+        const bool is_q = row < p.QH;
+        const int h = is_q ? row : row - p.QH;
+        const uint16_t *src = is_q ? p.q + t * p.q_stride : p.k + t * p.k_stride;
         float x[8];
         unpack8(*reinterpret_cast<const uint4 *>(src + (size_t)h * D + c0), x);
-        if (!is_v) {
+        {
             const uint16_t *w = is_q ? p.q_weight : p.k_weight;
             if (w) {
                 float sum = 0.0f;
@@ -274,21 +367,10 @@ __global__ __launch_bounds__(kRopeThreads) void norm_rope_kernel(RopeParams p)
         }
         if (is_q) {
             *reinterpret_cast<uint4 *>(p.q_out + t * p.q_out_stride + (size_t)h * D + c0) = pack8(x);
-        } else if (keep && !is_v) {
+        } else if (keep) {
             const size_t at = (((size_t)page * p.KVH + h) * p.page_size + place) * D + c0;
             if (F8) *reinterpret_cast<uint2 *>((uint8_t *)p.k_cache + at) = pack8_fp8(x, p.k_scale);
             else *reinterpret_cast<uint4 *>((uint16_t *)p.k_cache + at) = pack8(x);
-        } else if (keep) {
-            const size_t at = (((size_t)page * p.KVH + h) * D + c0) * p.page_size + place;
-            if (F8) {
-                const uint2 u = pack8_fp8(x, p.v_scale);
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    ((uint8_t *)p.v_cache)[at + (size_t)i * p.page_size] = (uint8_t)((i < 4 ? u.x : u.y) >> (8 * (i & 3)));
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) ((uint16_t *)p.v_cache)[at + (size_t)i * p.page_size] = (uint16_t)(__float_as_uint(x[i]) >> 16);
-            }
         }
     }
 }
@@ -372,10 +454,11 @@ extern "C" int lynx_qk_norm_rope(const uint16_t *q, int64_t q_stride, const uint
         (rc = check_rows(who, "q_out", q_out, q_out_stride, QH, D)) != LYNX_OK)
         return rc;
     RopeParams p = {q, k, v, q_weight, k_weight, q_stride, k_stride, v_stride, q_out_stride, positions, slots, freqs, q_out, k_cache,
-                    v_cache, eps, k_scale, v_scale, rot, interleaved ? 1 : 0, QH, KVH, num_pages * page_size, page_size};
+                    v_cache, eps, k_scale, v_scale, rot, interleaved ? 1 : 0, T, QH, KVH, num_pages * page_size, page_size,
+                    T <= kFewTokens ? 16 : kTurnTokens};
     const bool f8 = cache_format == LYNX_CACHE_FP8;
     auto kernel = D == 128 ? (f8 ? norm_rope_kernel<128, true> : norm_rope_kernel<128, false>)
                            : (f8 ? norm_rope_kernel<64, true> : norm_rope_kernel<64, false>);
-    hipLaunchKernelGGL(kernel, dim3(T), dim3(kRopeThreads), 0, (hipStream_t)stream, p);
+    hipLaunchKernelGGL(kernel, dim3(T + (T + p.turn - 1) / p.turn * KVH), dim3(kRopeThreads), 0, (hipStream_t)stream, p);
     return check_launch(who);
 }
