@@ -5,6 +5,9 @@ bits wide, so they have to lie in the first 64 KiB.  The language does not say w
 aligned to kStageAlign and the kernel's other arrays are smaller than that together: whatever lies ahead of or between
 the buffers moves the end of the segment by a whole kStageAlign, and the segment's size shows it.
 
+The attention kernel's four LDS buffers for blocks of the cache are filled by such loads too: aligned to ATTENTION_ALIGN, which is more
+than the kernel's other arrays take together.
+
 Waits: a wave reports its pieces of a chunk of token rows at a barrier, before which they must have landed.  The kernel waits
 until at most as many loads are outstanding as it has issued behind them, a number that follows from its source as long as
 the compiler neither drops nor merges loads.  They are counted again in the machine code, ahead of every barrier behind a
@@ -27,6 +30,8 @@ KERNEL = "ffn_kernel"
 WIDE = "ffn_wide_kernel"
 STAGE_END = 65536     # 2 * kStageBuffer
 STAGE_ALIGN = 4096    # kStageAlign
+ATTENTION = "attn_kernel"
+ATTENTION_ALIGN = 16384    # kLdsAlign
 
 
 def _run(tool, *args, cwd=None):
@@ -34,7 +39,7 @@ def _run(tool, *args, cwd=None):
 
 
 def code_object_texts(lib_path: str):
-    """(metadata notes, disassembly) of every gfx950 code object in the library that holds the kernel."""
+    """(metadata notes, disassembly) of every gfx950 code object in the library that holds one of the kernels."""
     with tempfile.TemporaryDirectory() as d:
         os.symlink(os.path.abspath(lib_path), os.path.join(d, "lib.so"))   # (the extracted objects land beside it)
         _run("llvm-objdump", "--offloading", "lib.so", cwd=d)
@@ -42,7 +47,7 @@ def code_object_texts(lib_path: str):
             if not name.endswith("gfx950"):
                 continue
             notes = _run("llvm-readelf", "--notes", name, cwd=d)
-            if KERNEL in notes:
+            if KERNEL in notes or ATTENTION in notes:
                 yield notes, _run("llvm-objdump", "-d", name, cwd=d)
 
 
@@ -53,6 +58,16 @@ def check_placement(notes: str) -> int:
     for size, name in kernels:
         if not STAGE_END <= int(size) < STAGE_END + STAGE_ALIGN:
             raise RuntimeError(f"{name}: {size} bytes of LDS: the buffers for token rows do not lie in the first {STAGE_END}")
+    return len(kernels)
+
+
+def check_attention_placement(notes: str) -> int:
+    """Raises if a buffer of the attention kernel can reach past STAGE_END; the number of kernels looked at."""
+    kernels = re.findall(r"\.group_segment_fixed_size:\s*(\d+)(?:(?!\.group_segment_fixed_size).)*?\.name:\s*(\S*" + ATTENTION + r"\S*)",
+                         notes, re.S)
+    for size, name in kernels:
+        if int(size) >= STAGE_END + ATTENTION_ALIGN:
+            raise RuntimeError(f"{name}: {size} bytes of LDS: the buffers for blocks of the cache do not lie in the first {STAGE_END}")
     return len(kernels)
 
 
@@ -184,10 +199,11 @@ def check_operands(listing: str) -> int:
 
 
 def check(lib_path: str) -> None:
-    kernels = barriers = products = 0
+    kernels = barriers = products = attention = 0
     for notes, listing in code_object_texts(lib_path):
         kernels += check_placement(notes)
         barriers += check_waits(listing)
         products += check_operands(listing)
-    if kernels == 0 or barriers < kernels or products == 0:
-        raise RuntimeError(f"{lib_path}: {kernels} kernels, {barriers} barriers and {products} products found: the checks do not read this library")
+        attention += check_attention_placement(notes)
+    if kernels == 0 or barriers < kernels or products == 0 or attention == 0:
+        raise RuntimeError(f"{lib_path}: {kernels} kernels, {barriers} barriers, {products} products and {attention} attention kernels found: the checks do not read this library")

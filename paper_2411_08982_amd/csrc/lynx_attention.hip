@@ -41,12 +41,13 @@ struct AttnParams {
     int window, sinks;
     int parts;                          // parts that the contexts of all tiles together are cut into, per key head
     float *part_o, *part_ml;            // workspace: unfinished rows
-    int narrow;                         // requests of more rows are left to attn_tiles_kernel
-    int wide_parts;                     // attn_tiles_kernel: parts that all its tiles' contexts are cut into, per key head
+    int narrow;                         // requests of more rows are left to the tiles of 128 rows
+    int wide_parts;                     // tiles of 128 rows: parts that all their contexts are cut into, per key head
     float *wide_o, *wide_ml;
     int prefix_blocks, prefix_splits;   // whole blocks of the shared prefix, and the parts that they are cut into
     float *prefix_o, *prefix_ml;        // the parts of all rows,
     float *own_o, *own_ml;              // and what the rows behind the prefix see of their own sequences
+    unsigned prefix_groups, tile_groups; // workgroups of the prefix's tiles and of the others
 };
 
 // Page (index in a row of the table) of the 16 tokens from 16 * group on: group / (page_size / 16), by multiplication.
@@ -103,39 +104,52 @@ struct Line {
     unsigned ends[LYNX_MAX_REQUESTS];       // where each request's blocks end on the line
     unsigned long long what[LYNX_MAX_REQUESTS];   // each request's first row (17 bits), rows (17 bits) and length (30 bits)
     unsigned sum[kAttnWaves];
+    float work[kAttnWaves];
 };
 // Blocks of each tile of a request: those that its last rows and its first see together, so no tile has more; one at least.
 __device__ __forceinline__ unsigned blocks_per_tile(const AttnParams &p, int n, int seq)
 {
     return (unsigned)max(blocks_of(p, seq - n, max(seq - n, 0), seq - 1).count, 1);
 }
-// Fills line.ends; the length of the line.
+// Fills line.ends; the length of the line.  (Row ranges that overlap, which is no batch, may make it longer than 32 bits: then it is 0.)
 __device__ __forceinline__ unsigned lay_out(const AttnParams &p, Line &line)
 {
     const int lane = lane_id(), wv = wave_id();
     const int per = (p.B + kAttnThreads - 1) / kAttnThreads, b0 = threadIdx.x * per;
     unsigned sum[kMaxPerThread], total = 0;
+    float work = 0.0f;
 #pragma unroll
     for (int i = 0; i < kMaxPerThread; ++i) {
         if (i < per && b0 + i < p.B) {
             int first, n, seq;
             request_of(p, b0 + i, first, n, seq);
             const unsigned tiles = n * p.G <= p.narrow ? (unsigned)(n * p.G + kRows - 1) / kRows : 0u;
-            if (tiles > 0) total += tiles * blocks_per_tile(p, n, seq);
+            if (tiles > 0) {
+                const unsigned blocks = blocks_per_tile(p, n, seq);
+                total += tiles * blocks;
+                work += (float)tiles * (float)blocks;
+            }
             line.what[b0 + i] = (unsigned long long)first << 47 | (unsigned long long)n << 30 | (unsigned)seq;
         }
         sum[i] = total;
     }
     unsigned before = (unsigned)wave_prefix_sum_i32((int)total);
-    if (lane == kWave - 1) line.sum[wv] = before;
+    work = wave_sum(work);
+    if (lane == kWave - 1) {
+        line.sum[wv] = before;
+        line.work[wv] = work;
+    }
     before -= total;
     __syncthreads();
     unsigned all = 0;
+    work = 0.0f;
 #pragma unroll
     for (int w = 0; w < kAttnWaves; ++w) {
         before += w < wv ? line.sum[w] : 0u;
         all += line.sum[w];
+        work += line.work[w];
     }
+    if (work > 2147483648.0f) all = 0;
 #pragma unroll
     for (int i = 0; i < kMaxPerThread; ++i)
         if (i < per && b0 + i < p.B) line.ends[b0 + i] = before + sum[i];
@@ -217,7 +231,7 @@ struct RowState {
 // A block of 64 tokens, in parts so that the next block's loads are under way while this one's products run: page numbers, keys, first
 // product; values, softmax and second product.
 // A bf16 block is two halves of 32 tokens, an 8-bit block is one piece: 16 bytes of a channel are 8 or 16 tokens of each of the four
-// lanes of a row.  Both halves' values are asked for together: with pages of 64 tokns they are the two halves of the same cache lines, and
+// lanes of a row.  Both halves' values are asked for together: with pages of 64 tokens they are the two halves of the same cache lines, and
 // asked for a step apart each line was read twice (256 requests of 1600 tokens, pages of 64: 3.5 TB/s).
 template <int D, bool F8>
 struct Step {
@@ -414,19 +428,27 @@ __device__ __forceinline__ void finish_row(const AttnParams &p, int t, int head,
 // LDS, and when all waves are through, the parts of each tile are joined: to the finished rows, or to a part in the workspace if
 // the tile goes on in another workgroup.  (With all four waves on one tile after the other, each with its round trips for lengths,
 // queries and page numbers, 256 requests with an 8-bit cache took 137 us where this takes 118.)
-template <int D, bool F8>
-__global__ __launch_bounds__(kAttnThreads, 2) void attn_rows_kernel(AttnParams p)
+constexpr int kRecords = 2 * kAttnWaves;
+struct RowsShared {
+    Line line;
+    unsigned rec[kRecords];                         // begin of the tile that the part belongs to
+    float sm[kRecords][kRows], sl[kRecords][kRows];
+};
+// part(k): 16 rows of D floats of LDS.
+template <int D, bool F8, typename Parts>
+__device__ __forceinline__ void rows_of(const AttnParams &p, unsigned x, int h, RowsShared &sh, const Parts &part_of)
 {
     typedef Step<D, F8> S;
-    constexpr int kRecords = 2 * kAttnWaves;
     constexpr unsigned kNone = 0xffffffffu;
-    __shared__ Line line;
-    __shared__ unsigned rec[kRecords];              // begin of the tile that the part belongs to
-    __shared__ float sm[kRecords][kRows], sl[kRecords][kRows];
-    __shared__ __align__(16) float so[kRecords][kRows][D + 4];
-    const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id()), h = blockIdx.y;
+    Line &line = sh.line;
+    unsigned(&rec)[kRecords] = sh.rec;
+    float(&sm)[kRecords][kRows] = sh.sm;
+    float(&sl)[kRecords][kRows] = sh.sl;
+    const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
     const unsigned total = lay_out(p, line), length = length_of(p, total);
-    const unsigned from = min(blockIdx.x * length, total), to = min(from + length, total);
+    const unsigned from = min(x * length, total), to = min(from + length, total);
+    // (four channels of a row stand at their place xor the row: the lanes that write have one place of all 16 rows)
+    const auto place = [&](int k, int row, int c) -> f32x4 & { return *reinterpret_cast<f32x4 *>(part_of(k) + row * D + (c / 4 ^ row) * 4); };
     if (from >= to) return;
     if (lane < 2) rec[2 * wv + lane] = kNone;
     const unsigned quarter = (length + kAttnWaves - 1) / kAttnWaves;
@@ -493,7 +515,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_rows_kernel(AttnParams p
             }
             if (lane == 0) rec[k] = f.begin;
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t) *reinterpret_cast<f32x4 *>(&so[k][lane & 15][t * 16 + (lane >> 4) * 4]) = s.o[t];
+            for (int t = 0; t < D / 16; ++t) place(k, lane & 15, t * 16 + (lane >> 4) * 4) = s.o[t];
         }
     }
     __syncthreads();
@@ -524,14 +546,14 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_rows_kernel(AttnParams p
                 const float e = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[w][orow] - m);
                 l += e * sl[w][orow];
 #pragma unroll
-                for (int i = 0; i < D / 64; ++i) o[i] += *reinterpret_cast<const f32x4 *>(&so[w][orow][c0 + 4 * i]) * e;
+                for (int i = 0; i < D / 64; ++i) o[i] += place(w, orow, c0 + 4 * i) * e;
             }
             if (begin >= from && begin + f.count <= to) {
                 const int tok = token_of(p, ro);
                 finish_row<D>(p, f.first + tok, h * p.G + ro - tok * p.G, behind_prefix(p, f.seq - f.n), c0, 4, m, l, o);
             } else {
                 // (a workgroup cuts two tiles at most: the one it begins inside, and the one it ends in)
-                const size_t part = ((size_t)(2 * blockIdx.x + (begin >= from ? 1 : 0)) * p.KVH + h) * kRows + orow;
+                const size_t part = ((size_t)(2 * x + (begin >= from ? 1 : 0)) * p.KVH + h) * kRows + orow;
 #pragma unroll
                 for (int i = 0; i < D / 64; ++i) *reinterpret_cast<f32x4 *>(p.part_o + part * D + c0 + 4 * i) = o[i];
                 if (c0 == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * part) = make_float2(m, l);
@@ -546,19 +568,19 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_rows_kernel(AttnParams p
 // parts), so there a tile's rows are spread over several workgroups, and the parts of a row over what is left of the workgroup's D / 4-lane
 // groups, which meet in LDS.
 template <int D>
-__global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p)
+__device__ __forceinline__ void join_rows(const AttnParams &p, unsigned cut_index, int h, int slice, int slices)
 {
     constexpr int L = D / 4, NG = kAttnThreads / L;         // lanes of a group (4 channels each), groups
     __shared__ Line line;
     __shared__ float sm[NG], sl[NG];
     __shared__ __align__(16) float4 so[NG][L];
-    const unsigned total = lay_out(p, line), length = length_of(p, total), cut = (blockIdx.x + 1) * length;
+    const unsigned total = lay_out(p, line), length = length_of(p, total), cut = (cut_index + 1) * length;
     if (cut >= total) return;
     const Place f = place_of(p, line, cut);
     if (f.begin == cut || f.begin + length < cut) return;          // between two tiles, or not the first cut of this one
-    const int h = blockIdx.y, slice = blockIdx.z, slices = gridDim.z, here = min(f.n * p.G - f.tile * kRows, kRows);
+    const int here = min(f.n * p.G - f.tile * kRows, kRows);
     const int mine = (here - slice + slices - 1) / slices;        // of the tile's rows, those of this workgroup
-    const int parts = (int)((f.begin + f.count - 1) / length) - (int)blockIdx.x + 1;
+    const int parts = (int)((f.begin + f.count - 1) / length) - (int)cut_index + 1;
     const int grp = threadIdx.x / L, lane = threadIdx.x % L;
     for (int done = 0; done < mine; done += NG) {
         int width = 1;                                              // rows at a time: a power of two
@@ -570,7 +592,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p)
 #pragma unroll 4
         for (int i = sub; i < parts; i += NG / width) {
             // the first part is the last of its workgroup unless the tile begins where the workgroup does
-            const unsigned x = blockIdx.x + i;
+            const unsigned x = cut_index + i;
             const size_t part = ((size_t)(2 * x + (f.begin >= x * length ? 1 : 0)) * p.KVH + h) * kRows + (real ? orow : slice);
             const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * part);
             const f32x4 u = *reinterpret_cast<const f32x4 *>(p.part_o + part * D + 4 * lane);
@@ -653,7 +675,7 @@ __device__ __forceinline__ bool find_part(const AttnParams &p, int x, FindShared
 #pragma unroll
     for (int w = 0; w < kAttnWaves; ++w) work += sh.work[w];
     // (a little more than the quotient: the sum is rounded, and there are no more than p.wide_parts + tiles workgroups)
-    const int chunk = max(kMinChunk, (int)(work * 1.0001f / (float)p.wide_parts) + 1);
+    const int chunk = max(kMinChunk, (int)fminf(work * 1.0001f / (float)p.wide_parts, 1e9f) + 1);
     int nx = 0, nc = 0;
 #pragma unroll
     for (int i = 0; i < kMaxPerThread; ++i) {
@@ -710,7 +732,7 @@ __device__ __forceinline__ float half_sum(float v)
 
 // A block of 64 tokens on its way from the pages into LDS, 16 bytes per load and lane.  Each of the block's four groups of 16 tokens lies
 // in one page; what one load instruction brings is of one group, so that its address is a scalar and a constant of the lane.
-//   keys [64][D]: row m holds token 16 (m / 16) + (m % 16 with bits 2 and 3 exchanged), see attn_tiles_kernel; the 16-byte pieces of
+//   keys [64][D]: row m holds token 16 (m / 16) + (m % 16 with bits 2 and 3 exchanged): the lane's scores are then of consecutive tokens; the 16-byte pieces of
 //   a row stand at their place xor (m & 7);
 //   values [4 groups][D][2 pieces]: wave w brings group w; the two pieces of a channel change places where bit 2 of it is set.
 // (The lanes of a fragment read one column of pieces, which would all lie in the same banks.)
@@ -831,22 +853,20 @@ __device__ __forceinline__ void blocks_ready()
 // A turn of the loop has the second product of one block and the first of the next, whose matrix instructions stand between the VALU
 // instructions of the softmax.  In LDS at a turn's start: its values and the next keys; on their way during it: the next values and
 // the keys after next.
-// PREFIX: the rows are those of the whole batch, whatever request they belong to, and the context is the shared prefix's whole blocks,
+// prefix: the rows are those of the whole batch, whatever request they belong to, and the context is the shared prefix's whole blocks,
 // which all of them see; every row's part is left in the workspace.
-template <int D, bool F8, bool PREFIX>
-__global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams p)
+template <int D, bool F8>
+__device__ __forceinline__ void tile_of(const AttnParams &p, bool prefix, int x, int h, u32x4 (&kbuf0)[kBlock * D / 8], u32x4 (&vbuf0)[kBlock * D / 8],
+                                        u32x4 (&kbuf1)[kBlock * D / 8], u32x4 (&vbuf1)[kBlock * D / 8])
 {
     typedef BlockLoad<D, F8> B;
     constexpr int NQ = D / 16, NV = D / 32, kAhead = 4;     // fragments are read from LDS four products ahead
-    // Four arrays and nothing else: loads into LDS reach its first 64 KiB, and which of two buffers is meant has to be known when
-    // this is compiled, for a read of one not to wait for loads into the other.
-    __shared__ __align__(16) u32x4 kbuf0[kBlock * D / 8], vbuf0[kBlock * D / 8], kbuf1[kBlock * D / 8], vbuf1[kBlock * D / 8];
-    static_assert(sizeof(FindShared) <= sizeof kbuf0 && 4 * sizeof kbuf0 <= 65536, "LDS");
-    const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id()), h = blockIdx.x % p.KVH, x = blockIdx.x / p.KVH;
+    static_assert(sizeof(FindShared) <= sizeof kbuf0, "LDS");
+    const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
     constexpr int kFar = 1 << 30;                   // behind every token of a prefix
     Part f;
     int first, n, seq;
-    if (PREFIX) {
+    if (prefix) {
         f = {0, x / p.prefix_splits, x % p.prefix_splits, p.prefix_splits, 0};
         first = 0;
         n = p.T;
@@ -862,9 +882,9 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
     const int pos = real ? base + tok : -1;
     const int tmin = max(base + token_of(p, f.tile * kTileRows), 0), tmax = base + token_of(p, min(f.tile * kTileRows + kTileRows, rows) - 1);
     const int pmin = max(base + token_of(p, r0), 0), pmax = r0 < rows ? base + token_of(p, min(r0 + kWaveRows, rows) - 1) : -1;    // of the wave's rows
-    const Blocks blocks = PREFIX ? Blocks{0, 0, p.prefix_blocks} : blocks_of(p, base, tmin, tmax);
+    const Blocks blocks = prefix ? Blocks{0, 0, p.prefix_blocks} : blocks_of(p, base, tmin, tmax);
     const int per = (blocks.count + f.splits - 1) / f.splits, i0 = f.split * per, i1 = min(i0 + per, blocks.count);
-    const int32_t *pages = PREFIX ? p.prefix_table : p.table + (size_t)f.b * p.max_pages;
+    const int32_t *pages = prefix ? p.prefix_table : p.table + (size_t)f.b * p.max_pages;
     const auto block = [&](int i) { return blocks.at(min(i, i1 - 1)); };
 
     B load(p);
@@ -1044,30 +1064,60 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tiles_kernel(AttnParams 
     for (int t = 0; t < D / 32; ++t)
 #pragma unroll
         for (int j = 0; j < 4; ++j) c[4 * t + j] = {o[t][4 * j], o[t][4 * j + 1], o[t][4 * j + 2], o[t][4 * j + 3]};
-    if (!PREFIX && f.splits == 1) {
+    if (!prefix && f.splits == 1) {
         finish_row<D>(p, first + tok, head, behind_prefix(p, base), hf * 4, 8, m, l, c);
     } else {
-        const size_t part = ((size_t)(PREFIX ? f.tile * f.splits + f.split : f.item + f.split) * p.KVH + h) * kTileRows + (r - f.tile * kTileRows);
-        float *dst = (PREFIX ? p.prefix_o : p.wide_o) + part * D + hf * 4;
+        const size_t part = ((size_t)(prefix ? f.tile * f.splits + f.split : f.item + f.split) * p.KVH + h) * kTileRows + (r - f.tile * kTileRows);
+        float *dst = (prefix ? p.prefix_o : p.wide_o) + part * D + hf * 4;
 #pragma unroll
         for (int k = 0; k < D / 8; ++k) *reinterpret_cast<f32x4 *>(dst + k * 8) = c[k];
-        if (hf == 0) *reinterpret_cast<float2 *>((PREFIX ? p.prefix_ml : p.wide_ml) + 2 * part) = make_float2(m, l);
+        if (hf == 0) *reinterpret_cast<float2 *>((prefix ? p.prefix_ml : p.wide_ml) + 2 * part) = make_float2(m, l);
     }
 }
 
-// Joins the parts of the tiles of attn_tiles_kernel that are cut: D / 4 lanes to a row.
+// One launch for all of a call: the prefix's tiles, the tiles of requests of many rows, and the line of the others, whose reading of the
+// cache stands beside the tiles' products (three launches one after the other: prefix of 8011, 100 requests, 8-bit cache 94 us,
+// this 82; 40 mixed requests of D = 64 86 us, this 72).
+constexpr int kLdsAlign = 16384;
+template <int D, bool F8, bool TILES>
+__global__ __launch_bounds__(kAttnThreads, 2) void attn_kernel(AttnParams p)
+{
+    // Loads into LDS reach its first 64 KiB, so these four arrays have to come first.  They are aligned to more than the rest of the LDS
+    // takes: if anything stood in front of one, the kernel's LDS would be larger by a whole kLdsAlign, which the build looks for (with
+    // D = 64 all of the LDS is less than 64 KiB).  They are four, since which of two buffers is meant has to be known when this is compiled, for a read of one not to wait for loads
+    // into the other.
+    __shared__ __align__(D == 128 ? kLdsAlign : 1024) u32x4 kbuf0[kBlock * D / 8], vbuf0[kBlock * D / 8], kbuf1[kBlock * D / 8], vbuf1[kBlock * D / 8];
+    __shared__ RowsShared rows;
+    static_assert(4 * sizeof kbuf0 <= 65536 && 2 * kRows * D * 4 == sizeof kbuf0 && sizeof rows < kLdsAlign, "LDS");
+    unsigned x = blockIdx.x;
+    if (TILES) {
+        const bool prefix = x < p.prefix_groups;
+        if (!prefix) x -= p.prefix_groups;
+        if (prefix || x < p.tile_groups) {
+            tile_of<D, F8>(p, prefix, x / p.KVH, x % p.KVH, kbuf0, vbuf0, kbuf1, vbuf1);
+            return;
+        }
+        x -= p.tile_groups;
+    }
+    rows_of<D, F8>(p, x / p.KVH, x % p.KVH, rows, [&](int k) {
+        float *const half = reinterpret_cast<float *>(k < 4 ? (k < 2 ? kbuf0 : vbuf0) : (k < 6 ? kbuf1 : vbuf1));
+        return half + (k & 1) * (kRows * D);
+    });
+}
+
+// Joins the parts of the tiles of 128 rows that are cut: D / 4 lanes to a row.
 constexpr int kTileSlices = 4;
 template <int D>
-__global__ __launch_bounds__(kAttnThreads) void attn_join_tiles_kernel(AttnParams p)
+__device__ __forceinline__ void join_tile(const AttnParams &p, int x, int h, int slice)
 {
     constexpr int L = D / 4, NG = kAttnThreads / L;
     __shared__ FindShared sh;
     Part f;
-    if (!find_part<true>(p, blockIdx.x, sh, f)) return;
+    if (!find_part<true>(p, x, sh, f)) return;
     int first, n, seq;
     request_of(p, f.b, first, n, seq);
-    const int h = blockIdx.y, lane = threadIdx.x % L, here = min(n * p.G - f.tile * kTileRows, kTileRows);
-    for (int row = blockIdx.z * (kTileRows / kTileSlices) + threadIdx.x / L; row < min((int)(blockIdx.z + 1) * (kTileRows / kTileSlices), here); row += NG) {
+    const int lane = threadIdx.x % L, here = min(n * p.G - f.tile * kTileRows, kTileRows);
+    for (int row = slice * (kTileRows / kTileSlices) + threadIdx.x / L; row < min((slice + 1) * (kTileRows / kTileSlices), here); row += NG) {
         const size_t part = ((size_t)f.item * p.KVH + h) * kTileRows + row, step = (size_t)p.KVH * kTileRows;
         float m = -INFINITY, l = 0.0f;
         f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -1084,6 +1134,22 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_tiles_kernel(AttnParam
         const int ro = f.tile * kTileRows + row, tok = token_of(p, ro);
         f32x4 own[1] = {o};
         finish_row<D>(p, first + tok, h * p.G + ro - tok * p.G, behind_prefix(p, seq - n), 4 * lane, 4, m, l, own);
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p, unsigned line_groups, int slices)
+{
+    unsigned x = blockIdx.x;
+    if (x < line_groups) {
+        const int slice = x % slices;
+        x /= slices;
+        join_rows<D>(p, x / p.KVH, x % p.KVH, slice, slices);
+    } else {
+        x -= line_groups;
+        const int slice = x % kTileSlices;
+        x /= kTileSlices;
+        join_tile<D>(p, x / p.KVH, x % p.KVH, slice);
     }
 }
 
@@ -1126,8 +1192,8 @@ __global__ __launch_bounds__(kAttnThreads) void attn_finish_kernel(AttnParams p)
 
 // Requests of up to this many rows are read by tiles of 16 rows, others by tiles of 128.
 constexpr int kNarrowRows = 64;
-// What the workspace holds: rows of unfinished tiles with their maxima and sums.  attn_rows_kernel leaves two tiles per workgroup.
-// attn_tiles_kernel: a tile that is cut has more than `chunk` blocks, so its parts are fewer than twice blocks / chunk, all such
+// What the workspace holds: rows of unfinished tiles with their maxima and sums.  A workgroup's length of the line leaves two tiles.
+// Tiles of 128 rows: a tile that is cut has more than `chunk` blocks, so its parts are fewer than twice blocks / chunk, all such
 // parts fewer than twice wide_parts, and such tiles at most wide_parts.
 // The prefix's tiles leave every row's parts, and the rows behind the prefix their own.
 struct AttnSpace {
@@ -1195,31 +1261,27 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
                     (float *)(ws + w.wide_ml_off), prefix_len / kBlock, w.prefix_splits, (float *)(ws + w.prefix_o_off), (float *)(ws + w.prefix_ml_off),
                     (float *)(ws + w.own_o_off), (float *)(ws + w.own_ml_off)};
     const bool f8 = cache_format == LYNX_CACHE_FP8;
-    auto kernel = D == 128 ? (f8 ? attn_rows_kernel<128, true> : attn_rows_kernel<128, false>)
-                           : (f8 ? attn_rows_kernel<64, true> : attn_rows_kernel<64, false>);
-    if (p.prefix_blocks > 0) {
-        auto prefix_kernel = D == 128 ? (f8 ? attn_tiles_kernel<128, true, true> : attn_tiles_kernel<128, false, true>)
-                                      : (f8 ? attn_tiles_kernel<64, true, true> : attn_tiles_kernel<64, false, true>);
-        hipLaunchKernelGGL(prefix_kernel, dim3((unsigned)KVH * w.prefix_tiles * w.prefix_splits), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
-    }
-    if (wide) {
-        // tiles: sum of ceil(rows / 128) over requests of more than kNarrowRows rows
-        const int tiles = (int)((int64_t)T * G / kTileRows) + (int)std::min<int64_t>(B, (int64_t)T * G / kNarrowRows);
-        auto tiles_kernel = D == 128 ? (f8 ? attn_tiles_kernel<128, true, false> : attn_tiles_kernel<128, false, false>)
-                                     : (f8 ? attn_tiles_kernel<64, true, false> : attn_tiles_kernel<64, false, false>);
-        hipLaunchKernelGGL(tiles_kernel, dim3((unsigned)KVH * (tiles + w.wide_parts)), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
-        hipLaunchKernelGGL((D == 128 ? attn_join_tiles_kernel<128> : attn_join_tiles_kernel<64>), dim3(std::min(tiles, w.wide_parts), KVH, kTileSlices),
-                           dim3(kAttnThreads), 0, (hipStream_t)stream, p);
-    }
-    hipLaunchKernelGGL(kernel, dim3(w.parts, KVH), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
+    const dim3 threads(kAttnThreads);
+    hipStream_t st = (hipStream_t)stream;
+    // tiles: at most the sum of ceil(rows / 128) over requests of more than kNarrowRows rows
+    const unsigned tiles = wide ? (unsigned)((int64_t)T * G / kTileRows + std::min<int64_t>(B, (int64_t)T * G / kNarrowRows)) : 0u;
+    p.prefix_groups = p.prefix_blocks > 0 ? (unsigned)KVH * w.prefix_tiles * w.prefix_splits : 0u;
+    p.tile_groups = wide ? KVH * (tiles + w.wide_parts) : 0u;
+    const bool any_tiles = p.prefix_groups + p.tile_groups > 0;
+    auto kernel = D == 128 ? (f8 ? (any_tiles ? attn_kernel<128, true, true> : attn_kernel<128, true, false>)
+                                 : (any_tiles ? attn_kernel<128, false, true> : attn_kernel<128, false, false>))
+                           : (f8 ? (any_tiles ? attn_kernel<64, true, true> : attn_kernel<64, true, false>)
+                                 : (any_tiles ? attn_kernel<64, false, true> : attn_kernel<64, false, false>));
+    hipLaunchKernelGGL(kernel, dim3(p.prefix_groups + p.tile_groups + (unsigned)KVH * w.parts), threads, 0, st, p);
     // a request's parts are w.parts / B on average: where they are many, a tile's rows go to four workgroups (one request of 9001 tokens:
     // 15 -> 4.4 us); else to one, since most workgroups have nothing to join (64 requests: 6.3 -> 4.9 us)
     const int slices = std::max(1, std::min(4, w.parts / (2 * B)));
-    if (w.parts > 1)
-        hipLaunchKernelGGL((D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>), dim3(w.parts - 1, KVH, slices), dim3(kAttnThreads), 0, (hipStream_t)stream, p);
+    const unsigned line_groups = (unsigned)(w.parts - 1) * KVH * slices, tile_joins = std::min(tiles, (unsigned)w.wide_parts) * KVH * kTileSlices;
+    if (line_groups + tile_joins > 0)
+        hipLaunchKernelGGL((D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>), dim3(line_groups + tile_joins), threads, 0, st, p, line_groups, slices);
     if (p.prefix_blocks > 0)
         hipLaunchKernelGGL((D == 128 ? attn_finish_kernel<128> : attn_finish_kernel<64>), dim3((unsigned)(((int64_t)T * QH * (D / 4) + kAttnThreads - 1) / kAttnThreads)),
-                           dim3(kAttnThreads), 0, (hipStream_t)stream, p);
+                           threads, 0, st, p);
     return check_launch(who);
 }
 

@@ -10,6 +10,8 @@ import torch
 import attention_ref as ref
 import paper_2411_08982_amd as L
 from paper_2411_08982_amd import attention as A
+from paper_2411_08982_amd import check_code
+from paper_2411_08982_amd.build import LIB
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HEADER = os.path.join(ROOT, "include", "lynx", "attention.h")
@@ -153,3 +155,12 @@ def test_the_oracle_agrees_with_a_dense_computation():
     r = ref.kv_assign([15, 16, 3], [2, 1, -1], 4, 16, [[1, -1], [2, -1], [3, -1]], [9, 5, 4, 9, 9, 9], [1, 2])
     assert r["table"] == [[1, 5], [2, 4], [3, -1]] and r["ring"] == [9, 5, 4, 3, 9, 9] and r["ring_state"] == [3, 1]
     assert r["q_start"] == [0, 2, 3, 3] and r["slots"] == [31, 80, 64, -1] and r["seq_len"] == [17, 17, 0] and r["status"] == [0]
+
+
+@pytest.mark.skipif(not os.path.exists(LIB), reason="the library is not built")
+def test_block_buffers_lie_in_the_first_64_kib():
+    assert sum(check_code.check_attention_placement(notes) for notes, _ in check_code.code_object_texts(LIB)) == 8    # D, cache format, with tiles or without
+    notes = "\n  - .group_segment_fixed_size: %d\n    .name:           _ZN4lynx11attn_kernelILi128ELb0ELb1EEEvNS_10AttnParamsE\n"
+    assert check_code.check_attention_placement(notes % (65536 + 16383)) == 1
+    with pytest.raises(RuntimeError, match="first 65536"):
+        check_code.check_attention_placement(notes % (65536 + 16384))

@@ -150,6 +150,17 @@ def test_rows_that_see_nothing_and_lengths_that_lie():
     torch.cuda.synchronize()
 
 
+def test_row_ranges_that_overlap_beyond_all_bounds():
+    # 512 requests that each claim all rows, a million tokens long: 2^34 blocks to read, more than 32 bits count.  Nothing is read
+    B, T, pages = 1024, 4096, 1024
+    q_start = i32([0, T] * (B // 2) + [0])
+    cache = L.new_cache(2, 1, 1024, 64)
+    q = torch.zeros(T, 8, 64, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 7.0)
+    L.lynx_attention(q, *cache, torch.zeros(B, pages, dtype=torch.int32, device="cuda"), q_start, i32([pages * 1024] * B), 1, out=out)
+    assert bool((out == 7).all())
+
+
 def test_strided_rows():
     c = Case(MIXED, 6, 2, 64, 16, seed=10)
     out, _ = c.check()
