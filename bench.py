@@ -17,13 +17,15 @@ report with every configuration in it goes to stderr as a JSON line of its own, 
     the remap costs (mean ratio of the selected softmax mass after / before, share of tokens that keep their top-1);
   * `mixtral_T8`: the Mixtral-shaped layer at 8 tokens in detail (stage times, plain-read ceiling, FP8 / MXFP4 weights).
 With --config NAME it measures that one configuration (single layer, or --stack L layers): what the rocprofv3 summaries
-under profiles/ were taken from.
+under profiles/ were taken from.  With --stack and --attention CONTEXT the same stack is timed once more as whole decode
+layers: each MoE layer behind projections, norms and rotation, cache write and attention over CONTEXT tokens of a paged
+cache per request (field `attention`; the other fields stay those of the MoE layers alone).
 
 Successive steps of a single-layer measurement cycle over several resident copies of the layer's expert weights
 (distinct buffers, same router and tokens), as the layers of a model would: a step that re-read the very buffers of the
 step before would find a small configuration's experts in the 256 MB last-level cache and report a rate above HBM's.
 
-    python bench.py [--gpus 1] [--steps K] [--warmup W] [--config NAME --tokens T --preset P | --stack L]
+    python bench.py [--gpus 1] [--steps K] [--warmup W] [--config NAME --tokens T --preset P | --stack L [--attention C]]
 """
 from __future__ import annotations
 
@@ -39,6 +41,8 @@ if ROOT not in sys.path:
 
 HBM_PEAK_GBPS = 8000.0
 PRESET_NAMES = ("off", "moderate", "aggressive")
+HEADS = {"tiny": (8, 2, 64), "mixtral": (32, 8, 128), "qwen15moe": (16, 16, 128), "qwen3": (32, 4, 128)}   # query heads, key heads, channels
+PAGE_SIZE = 64
 
 
 def parse():
@@ -73,6 +77,12 @@ def parse():
                     help="with --config: time a chained stack of this many layers (own router and weights each, "
                          "x <- bf16(x + y) between them) as a whole, eagerly and as one HIP graph")
     ap.add_argument("--stack-layers", type=int, default=48, help="layers of the stack in the full report")
+    ap.add_argument("--attention", type=int, default=0, metavar="CONTEXT",
+                    help="with --stack: time whole decode layers as well, every request with CONTEXT tokens in a paged cache")
+    ap.add_argument("--shared-prefix", type=int, default=0, metavar="TOKENS",
+                    help="with --attention: the first TOKENS of every context are the same, in the same pages (up to the "
+                         "last whole page), and are read once for the batch")
+    ap.add_argument("--cache", default="bf16", choices=["bf16", "fp8"], help="with --attention: type of the cache")
     ap.add_argument("--report", default="", metavar="FILE", help="write the full report to this file as well")
     ap.add_argument("--pmc-calibration", action="store_true",
                     help="before the steps, run a plain 1 GiB read + 1 GiB write elementwise kernel three times: under "
@@ -80,7 +90,14 @@ def parse():
     ap.add_argument("--down-item-cap", type=int, default=0, help="tuning: down-projection work items the plan aims at")
     ap.add_argument("--down-item-units", type=int, default=0, help="tuning: most 64-row units per down work item")
     ap.add_argument("--down-k-waves", type=int, default=0, help="tuning: K slices of a down workgroup's waves")
-    return ap.parse_args()
+    args = ap.parse_args()
+    if args.attention < 0 or not 0 <= args.shared_prefix <= args.attention:
+        ap.error("--attention: a number of tokens, --shared-prefix at most as many")
+    if args.attention > 0 and (not args.config or args.stack <= 0):
+        ap.error("--attention goes with --config NAME --stack L")
+    if args.attention > 0 and args.config not in HEADS:
+        ap.error(f"--attention: {args.config} has no grouped-head attention here (of those that have: {', '.join(HEADS)})")
+    return args
 
 
 def expert_bytes(cfg, n_routed):
@@ -354,6 +371,109 @@ class Stack:
                 "top1_kept": round(float(np.mean([q[1] for q in ratios])), 4)}
 
 
+class DecodeStack:
+    """The layers of a Stack as whole decode layers: T requests with one new token each behind `context` cached ones."""
+
+    def __init__(self, stack, context, prefix, cache):
+        torch, L, cfg, T = stack.torch, stack.L, stack.cfg, stack.T
+        self.stack, self.context, self.prefix = stack, context, prefix
+        self.QH, self.KVH, self.D = QH, KVH, D = HEADS[cfg.name]
+        dt = torch.float8_e4m3fn if cache == "fp8" else torch.bfloat16
+        self.scales = dict(k_scale=1 / 64, v_scale=1 / 64) if cache == "fp8" else {}
+        g = torch.Generator(device="cuda").manual_seed(7)
+        rand = lambda *shape, scale=1.0: (torch.randn(shape, generator=g, device="cuda") * scale).to(torch.bfloat16)
+        i32 = lambda a: torch.as_tensor(a, dtype=torch.int32, device="cuda")
+        common = prefix // PAGE_SIZE
+        per_row = context // PAGE_SIZE + 1
+        held = -(-context // PAGE_SIZE)
+        pages = common + T * (per_row - common)
+        order = torch.randperm(pages, generator=g, device="cuda").to(torch.int32)
+        self.table = torch.cat([order[:common].expand(T, common), order[common:].view(T, per_row - common)], 1).contiguous()
+        ring = self.table[:, held:].reshape(-1)             # the last pages are free: the step takes them where it needs them
+        self.table[:, held:] = -1
+        self.ring = torch.cat([ring, ring.new_full((pages - ring.numel(),), -1)])
+        self.state = i32([0, ring.numel()])
+        self.prefix_table = self.table[0, :-(-prefix // PAGE_SIZE)].contiguous()
+        self.shared = common
+        self.ctx, self.new = i32([context] * T), i32([1] * T)
+        self.assigned = dict(q_start=i32([0] * (T + 1)), seq_len=i32([0] * T), positions=i32([0] * T), slots=i32([0] * T),
+                             ring_state=i32([0, 0]), status=i32([0]))
+        self.freqs = 1e6 ** (-torch.arange(0, D, 2, dtype=torch.float64, device="cuda") / D)
+        self.layers = []
+        for _ in stack.layers:
+            kc, vc = L.new_cache(pages, KVH, PAGE_SIZE, D, dt)
+            for c in (kc, vc):
+                for part in c.split(4096):
+                    part.copy_((torch.randn(part.shape, generator=g, device="cuda") * (8.0 if self.scales else 1.0)).to(dt))
+            self.layers.append((rand(cfg.H, (QH + 2 * KVH) * D, scale=cfg.H ** -0.5), rand(QH * D, cfg.H, scale=(QH * D) ** -0.5),
+                                1 + rand(D, scale=0.1), 1 + rand(D, scale=0.1), kc, vc))
+        self.qkv = torch.empty(T, (QH + 2 * KVH) * D, dtype=torch.bfloat16, device="cuda")
+        self.q, self.o = (torch.empty(T, QH, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        self.mid = torch.empty_like(stack.xs[0])
+        self.ws = L.new_attention_workspace(T, T, QH, KVH, D, prefix)
+        # bytes of the cache that a layer has to read: the shared prefix once
+        self.cache_bytes = (prefix + T * (context + 1 - prefix)) * 2 * KVH * D * (1 if self.scales else 2)
+
+    def assign(self):
+        self.stack.L.lynx_kv_assign(self.ctx, self.new, self.stack.T, PAGE_SIZE, self.table, self.ring, self.state, self.shared, out=self.assigned)
+
+    def attention(self, l):
+        """mid = x + the attention of layer l over x = xs[l]."""
+        L, torch, a, x = self.stack.L, self.stack.torch, self.assigned, self.stack.xs[l]
+        QH, KVH, D = self.QH, self.KVH, self.D
+        Wqkv, Wo, wq, wk, kc, vc = self.layers[l]
+        torch.mm(x, Wqkv, out=self.qkv)
+        q, k, v = (t.unflatten(1, (-1, D)) for t in self.qkv.split([QH * D, KVH * D, KVH * D], 1))
+        L.lynx_qk_norm_rope(q, k, v, a["positions"], a["slots"], self.freqs, kc, vc, wq, wk, q_out=self.q, **self.scales)
+        args = (self.q, kc, vc, self.table, a["q_start"], a["seq_len"], 1)
+        if self.prefix:
+            L.lynx_attention_prefix(*args, self.prefix_table, self.prefix, out=self.o, workspace=self.ws, **self.scales)
+        else:
+            L.lynx_attention(*args, out=self.o, workspace=self.ws, **self.scales)
+        torch.addmm(x, self.o.view(x.shape[0], QH * D), Wo, out=self.mid)
+
+    def chain(self, per_layer, moe=True):
+        s, cfg = self.stack, self.stack.cfg
+        self.assign()
+        for l, (Wr, bias, Wgu, Wdp, Sgu, Sdp) in enumerate(s.layers):
+            self.attention(l)
+            if not moe:
+                continue
+            alpha, beta, enable = per_layer[l]
+            b = s.L.lynx_moe_layer(self.mid, Wr, bias, Wgu, Wdp, cfg.F, cfg.k, alpha, beta, enable, Sgu, Sdp, cfg.n_shared, cfg.F_shared,
+                                   buffers=s.bufs[l][beta])
+            s.L.lynx_residual_add(self.mid, b.y, out=s.xs[l + 1])
+
+    def measure(self, per_layer, steps, warmup):
+        torch, s = self.stack.torch, self.stack
+        res = {}
+        for name, moe in (("us_graph", True), ("us_graph_attention", False)):
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                self.chain(per_layer, moe)
+            torch.cuda.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                self.chain(per_layer, moe)
+            for _ in range(max(1, warmup)):
+                g.replay()
+            torch.cuda.synchronize()
+            t0 = time.perf_counter()
+            for _ in range(steps):
+                g.replay()
+            torch.cuda.synchronize()
+            res[name] = round((time.perf_counter() - t0) * 1e6 / steps, 1)
+            del g
+        if int(self.assigned["status"]):
+            raise RuntimeError("lynx_kv_assign did not place every token")
+        return {"context": self.context, "shared_prefix": self.prefix, "cache": "fp8_e4m3" if self.scales else "bf16", "page_size": PAGE_SIZE,
+                "query_heads": self.QH, "key_heads": self.KVH, "channels": self.D, **res,
+                "tokens_per_s": round(s.T / (res["us_graph"] * 1e-6), 1),
+                "cache_bytes_per_layer": self.cache_bytes,
+                "cache_GBps_attention": round(self.cache_bytes * s.n / (res["us_graph_attention"] * 1e-6) / 1e9, 1)}
+
+
 def cpu_baseline_stack(stack, T, preset, torch, wl, n_cpu_layers):
     """The oracle (plain C, fp64, as it stands) on the first n_cpu_layers layers of the stack, chained like the GPU's
     (x <- bf16(x + y)), timed on the host cores; the whole stack is that times n_layers / n_cpu_layers."""
@@ -426,6 +546,9 @@ def stack_line(args, cfg, wl, torch, n_layers, T_list, presets, headline, table=
                         "launches_per_step": launches, "bytes_per_launch": best["expert_weight_bytes"] // launches,
                         "avg_launch_us": round(best["ffn_kernel_us"] / launches, 2),
                         "whole_stack_frac": best["stack_hbm_frac"], "whole_stack_GBps": best["expert_weight_GBps_graph"]}}
+    if args.attention:
+        out["attention"] = DecodeStack(stack, args.attention, args.shared_prefix, args.cache).measure([preset_args(wl, preset)] * n_layers,
+                                                                                                     args.steps, args.warmup)
     if cpu_layers:
         out["cpu_baseline"] = cpu_baseline_stack(stack, T, preset, torch, wl, cpu_layers)
     del stack

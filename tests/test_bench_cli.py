@@ -56,3 +56,10 @@ def test_the_line_of_the_full_report_is_short():
     assert all(line[k] == v for k, v in agreed.items())
     assert line["stack_us"]["T512_aggressive"] == 12345.6 and line["mixtral_T8_us"] == 120.5
     assert len(json.dumps(line)) < 4000
+
+
+def test_attention_options_that_do_not_fit_are_refused():
+    for bad in (["--attention", "64"], ["--config", "tiny", "--attention", "64"], ["--config", "dsv2lite", "--stack", "2", "--attention", "64"],
+                ["--config", "tiny", "--stack", "2", "--attention", "64", "--shared-prefix", "65"], ["--config", "tiny", "--stack", "2", "--shared-prefix", "1"]):
+        r = subprocess.run([sys.executable, os.path.join(ROOT, "bench.py"), *bad], capture_output=True, text=True)
+        assert r.returncode == 2 and "--attention" in r.stderr and r.stdout.strip() == "", bad

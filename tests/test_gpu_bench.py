@@ -57,3 +57,14 @@ def test_bench_router_options():
     assert "sigmoid-gated router" in d["config"]["workload"] and "group-limited router (2 of 4 groups)" in d["config"]["workload"]
     assert d["value"] > 0 and "cpu_baseline" not in d and "fp8_weights" not in d
     assert d["experts_invoked"]["after"] <= d["experts_invoked"]["before"]
+
+
+@pytest.mark.parametrize("options", [["--attention", "200"], ["--attention", "128", "--shared-prefix", "100", "--cache", "fp8"]])
+def test_bench_whole_decode_layers(options):
+    print("bench.py --config tiny --stack 2", *options, flush=True)
+    d = _run("--config", "tiny", "--tokens", "16", "--stack", "2", "--steps", "3", "--warmup", "1", *options)
+    a = d["attention"]
+    assert a["us_graph"] > a["us_graph_attention"] > 0 and a["context"] == int(options[1])
+    rows = 16 * 201 if len(options) == 2 else 100 + 16 * 29
+    assert a["cache_bytes_per_layer"] == rows * 2 * 2 * 64 * (2 if len(options) == 2 else 1)
+    assert set(d["stack"]) == {"off", "aggressive"} and d["value"] > 0        # the line's own fields are the MoE layers'
