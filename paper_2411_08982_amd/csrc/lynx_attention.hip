@@ -4,16 +4,16 @@
 // n new tokens times G: row r is token r / G, head r % G of the group.
 //
 // Products.  Both are taken transposed on the matrix cores, v_mfma_f32_16x16x32_bf16:  S^T = K Q^T and O^T = V^T P^T.  A result
-// fragment of S^T holds, in lane l, the scores of row l % 16 with 4 tokens; K's rows are handed in such an order that the fragments of
-// one step give every lane 8 (bf16 cache) or 16 (8-bit cache) CONSECUTIVE tokens, and these are exactly what the lane has to hold as operand
-// of the second product.  So the weights never leave their lane: no LDS, no exchange; running maximum, sum and the rescaling
-// of O^T are per lane (a row is one column of both results), and only the maximum is joined over the four lanes of a row.
-// V's operand wants those tokens of one channel: one 16-byte load from the transposed pages.
+// fragment of S^T holds, in lane l, the scores of row l % 16 with 4 consecutive tokens; two fragments give the lane 8 tokens, and in the
+// second product, whose terms may come in any order, these are what it holds of its operand.  So the weights never leave their
+// lane: no LDS, no exchange; running maximum, sum and the rescaling of O^T are per lane (a row is one column of both results), and
+// only the maximum is joined over the four lanes of a row.  V's operand wants those tokens of one channel: the transposed pages.
 //
 // Softmax in one pass: m = running maximum (of the scores times scale * log2 e), l = sum of 2^(s - m), O accumulates 2^(s - m) v; when
 // m grows, l and O are multiplied by 2^(m_old - m_new).  All in fp32.
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "lynx_attention.h"
 
@@ -201,15 +201,7 @@ __device__ __forceinline__ float row_sum(float v)
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// 16 bytes that this launch reads once: past the caches.  For loads that cover whole cache lines with one instruction, as those of the
-// values do (64 requests, 411 MB of bf16 cache: 79.6 -> 63.6 us); the keys' cover half lines, whose other half the hint would
-// have read again (a plain read of scattered pages: 5.9 TB/s without the hint either way, with it 6.8 for whole lines and 5.1 for
-// halves).
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ uint4 load_once(const void *at)
-{
-    return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(at)));
-}
 
 // 8 E4M3 codes as bf16 (exact).
 __device__ __forceinline__ bf16x8 widen8(uint2 c)
@@ -228,166 +220,275 @@ struct RowState {
     f32x4 o[D / 16];
 };
 
-// A block of 64 tokens, in parts so that the next block's loads are under way while this one's products run: page numbers, keys, first
-// product; values, softmax and second product.
-// A bf16 block is two halves of 32 tokens, an 8-bit block is one piece: 16 bytes of a channel are 8 or 16 tokens of each of the four
-// lanes of a row.  Both halves' values are asked for together: with pages of 64 tokens they are the two halves of the same cache lines, and
-// asked for a step apart each line was read twice (256 requests of 1600 tokens, pages of 64: 3.5 TB/s).
+// At most N of the loads that this wave has asked for are still on their way.
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// A block of 64 tokens of the cache on its way through a wave.  Keys and values come in units of 4 KiB (2 KiB for 8 bits and D = 64), first
+// those of the keys: all channels of 16 or 32 tokens, then those of the values: all tokens of 32 or 64 channels.  A unit goes from memory
+// into one of the wave's four places in LDS directly, 1 KiB by each load, and every load takes cache lines whole.  (A fragment takes 64
+// bytes of each of its 16 rows, of a token's key or a channel's values: loaded into registers as the products take them, that is half of
+// a line at a time.  32 requests of 4096 tokens with 4 key heads: 59.9 us so, 54.5 through LDS; 64 of 6000 with 8: 266 and 249.)
+// The loads carry the hint that the lines are used once (without it: 60.2 and 282 us).  As soon as a unit is read, the one four behind it
+// is asked for, so a wave has 16 KiB on their way (8 KiB for 8 bits and D = 64), a CU 128.
+// A row of a unit, 64 to 256 bytes, has its 16-byte pieces at their place xor a few bits of the row, for the 16 rows of a fragment to lie in
+// different banks.
 template <int D, bool F8>
 struct Step {
-    static constexpr int E = F8 ? 1 : 2;           // bytes of an element
-    static constexpr int H = F8 ? 1 : 2;           // pieces
-    static constexpr int NS = kBlock / 16 / H;     // fragments of S^T of a piece
-    static constexpr int LT = 4 * NS;              // consecutive tokens of a lane in a piece
-    static constexpr int KL = D * E / 64;          // 16-byte loads of a key row by its four lanes
+    static constexpr int E = F8 ? 1 : 2;                   // bytes of an element
+    static constexpr int kUnit = F8 && D == 64 ? 2048 : 4096;
+    static constexpr int NU = kBlock * D * E / kUnit;      // units of keys, and of values
+    static constexpr int NL = kUnit / 1024;                // loads of a unit
+    static constexpr int RK = D * E, RV = kBlock * E;      // bytes of a row: a token's key, a channel's values
+    static constexpr int PK = RK / 16, PV = RV / 16;       // pieces of it
+    static constexpr int KL = PK / 4;                      // pieces of a key that each of its four lanes takes
 
-    int kid[H], vid[H];                            // page numbers of the lane's key rows and of its run of tokens
-    unsigned there;                                // bit i: its run of piece i has a page
-    uint4 kw[H][NS][KL], vw[H][D / 16];
+    int t0, id[4];                                 // first token; page numbers of the four times 16 tokens
+    unsigned there;                                // which of the four have a page
+    const uint8_t *values;                         // the lane's place in the first 8 or 16 channels
 
-    // This lane's token for the first fragment of piece i (the others follow 4 apart), and the first of its run.
-    static __device__ __forceinline__ int key_token(int t0, int i) { return t0 + i * 32 + ((lane_id() & 15) >> 2) * LT + (lane_id() & 3); }
-    static __device__ __forceinline__ int run_token(int t0, int i) { return t0 + i * 32 + (lane_id() >> 4) * LT; }
+    static __device__ __forceinline__ int key_swizzle(int token) { return PK == 16 ? token & 15 : PK == 8 ? token & 7 : token >> 2 & 3; }
+    static __device__ __forceinline__ int value_swizzle(int channel) { return PV == 8 ? channel & 7 : channel >> 2 & 3; }
 
-    __device__ __forceinline__ void fetch_pages(const AttnParams &p, const int32_t *pages, int t0)
+    // What the table says of the pages.  Scalar loads: they are counted apart from those into LDS, and the compiler, which waits for all of
+    // these before a vector load's result, need not.
+    struct Pages {
+        int id[4];
+    };
+    static __device__ __forceinline__ Pages fetch_pages(const AttnParams &p, const int32_t *pages, int t0)
     {
-        const int last = p.max_pages - 1;
+        Pages s;
+        const auto *table = (const __attribute__((address_space(4))) int32_t *)pages;
 #pragma unroll
-        for (int i = 0; i < H; ++i) {
-            kid[i] = pages[min(page_of(p, key_token(t0, i) >> 4), last)];
-            vid[i] = pages[min(page_of(p, run_token(t0, i) >> 4), last)];
+        for (int g = 0; g < 4; ++g) s.id[g] = table[min(page_of(p, (t0 >> 4) + g), p.max_pages - 1)];
+        return s;
+    }
+    // Takes a block on.  (Tokens without a page are read from the first one and not seen.)
+    __device__ __forceinline__ void begin(const AttnParams &p, int h, int at, const Pages &pages)
+    {
+        const int lane = lane_id();
+        t0 = at;
+        there = 0u;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int known = (int)(page_of(p, (t0 >> 4) + g) < p.max_pages) & (int)((unsigned)pages.id[g] < (unsigned)p.num_pages);
+            id[g] = known ? pages.id[g] : 0;
+            there |= known ? 1u << g : 0u;
+        }
+        const int channel = lane / PV, piece = (lane % PV) ^ value_swizzle(channel), g = F8 ? piece : piece >> 1;
+        const int lo = g & 1 ? id[1] : id[0], hi = g & 1 ? id[3] : id[2];
+        values = (const uint8_t *)p.v + ((((size_t)(g & 2 ? hi : lo) * p.KVH + h) * D + channel) * p.page_size + place(p, g)) * E + (F8 ? 0 : (piece & 1) * 16);
+    }
+    // Place in its page of 16 tokens g
+    __device__ __forceinline__ int place(const AttnParams &p, int g) const
+    {
+        const int at = (t0 >> 4) + g;
+        return at * 16 - page_of(p, at) * p.page_size;
+    }
+
+    // Asks for unit n.
+    __device__ __forceinline__ void load(const AttnParams &p, int h, int n, u32x4 *to) const
+    {
+        const int lane = lane_id();
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const uint8_t *src;
+            if (n < NU) {
+                const int token = (n * NL + i) * (64 / PK), row = token % 16 + lane / PK;
+                src = (const uint8_t *)p.k + ((size_t)id[token / 16] * p.KVH + h) * ((size_t)p.page_size * RK) +
+                      (size_t)(place(p, token / 16) * RK) + (unsigned)(row * RK + ((lane % PK) ^ key_swizzle(row)) * 16);
+            } else {
+                src = values + (size_t)(((n - NU) * NL + i) * (64 / PV)) * (unsigned)(p.page_size * E);
+            }
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src, (__attribute__((address_space(3))) void *)(to + i * 64), 16, 0, 2);
         }
     }
 
-    // (tokens without a page are read from the first one and not seen)
-    __device__ __forceinline__ void fetch_keys(const AttnParams &p, int h, int t0)
+    // The fragments of a unit of keys, [16 tokens][KL pieces], and of a unit of values, [16 channels][the lane's four tokens of each 16],
+    // read from LDS.  (Written out together with their wait: before a read of its own the compiler would wait for all loads
+    // into LDS, since it does not follow which of them has come.)
+    static constexpr int NG = 4 / NU, NT = D / 16 / NU;
+    static __device__ __forceinline__ unsigned lds(const void *at) { return (unsigned)(size_t)(const __attribute__((address_space(3))) void *)at; }
+    static __device__ __forceinline__ void keys(const u32x4 *unit, u32x4 (&k)[NG][KL])
     {
+        const int row = lane_id() & 15, q = lane_id() >> 4;
+        unsigned at[KL];
 #pragma unroll
-        for (int i = 0; i < H; ++i) {
-            const int t = key_token(t0, i), place = t - page_of(p, t >> 4) * p.page_size;
-            const uint8_t *a = (const uint8_t *)p.k + (((size_t)((unsigned)kid[i] < (unsigned)p.num_pages ? kid[i] : 0) * p.KVH + h) * p.page_size + place) * (D * E) +
-                               (lane_id() >> 4) * 16;
-#pragma unroll
-            for (int j = 0; j < NS; ++j)
-#pragma unroll
-                for (int k = 0; k < KL; ++k) kw[i][j][k] = *reinterpret_cast<const uint4 *>(a + j * 4 * (D * E) + k * 64);
-        }
+        for (int j = 0; j < KL; ++j) at[j] = lds(unit) + row * RK + ((4 * j + q) ^ key_swizzle(row)) * 16;
+        if constexpr (KL == 4)
+            asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\ts_waitcnt lgkmcnt(0)"
+                         : "=&v"(k[0][0]), "=&v"(k[0][1]), "=&v"(k[0][2]), "=&v"(k[0][3]) : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]) : "memory");
+        else if constexpr (KL == 2)
+            asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %4 offset:%6\n\tds_read_b128 %3, %5 offset:%6\n\ts_waitcnt lgkmcnt(0)"
+                         : "=&v"(k[0][0]), "=&v"(k[0][1]), "=&v"(k[1][0]), "=&v"(k[1][1]) : "v"(at[0]), "v"(at[1]), "n"(16 * RK) : "memory");
+        else
+            asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:%3\n\ts_waitcnt lgkmcnt(0)"
+                         : "=&v"(k[0][0]), "=&v"(k[1][0]) : "v"(at[0]), "n"(16 * RK) : "memory");
     }
-    __device__ __forceinline__ void fetch_values(const AttnParams &p, int h, int t0)
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    typedef typename std::conditional<F8, unsigned, u32x2>::type Four;         // four tokens of a channel
+    static __device__ __forceinline__ void values_of(const u32x4 *unit, Four (&v)[NT][4])
     {
-        const uint8_t *a[H];
-        there = 0;
+        const int row = lane_id() & 15, q = lane_id() >> 4;
+        unsigned at[4];
 #pragma unroll
-        for (int i = 0; i < H; ++i) {
-            const int t = run_token(t0, i), page = page_of(p, t >> 4), place = t - page * p.page_size;
-            const bool known = (unsigned)vid[i] < (unsigned)p.num_pages;
-            there |= known && page < p.max_pages ? 1u << i : 0u;
-            a[i] = (const uint8_t *)p.v + ((((size_t)(known ? vid[i] : 0) * p.KVH + h) * D + (lane_id() & 15)) * p.page_size + place) * E;
+        for (int g = 0; g < 4; ++g)
+            at[g] = lds(unit) + row * RV + (F8 ? (g ^ value_swizzle(row)) * 16 + q * 4 : ((2 * g + (q >> 1)) ^ value_swizzle(row)) * 16 + (q & 1) * 8);
+#pragma unroll
+        for (int t = 0; t < NT; t += 2) {
+            if constexpr (F8)
+                asm volatile("ds_read_b32 %0, %8 offset:%12\n\tds_read_b32 %1, %9 offset:%12\n\tds_read_b32 %2, %10 offset:%12\n\tds_read_b32 %3, %11 offset:%12\n\t"
+                             "ds_read_b32 %4, %8 offset:%13\n\tds_read_b32 %5, %9 offset:%13\n\tds_read_b32 %6, %10 offset:%13\n\tds_read_b32 %7, %11 offset:%13\n\t"
+                             "s_waitcnt lgkmcnt(0)"
+                             : "=&v"(v[t][0]), "=&v"(v[t][1]), "=&v"(v[t][2]), "=&v"(v[t][3]), "=&v"(v[t + 1][0]), "=&v"(v[t + 1][1]), "=&v"(v[t + 1][2]), "=&v"(v[t + 1][3])
+                             : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(t * 16 * RV), "n"((t + 1) * 16 * RV) : "memory");
+            else
+                asm volatile("ds_read_b64 %0, %8 offset:%12\n\tds_read_b64 %1, %9 offset:%12\n\tds_read_b64 %2, %10 offset:%12\n\tds_read_b64 %3, %11 offset:%12\n\t"
+                             "ds_read_b64 %4, %8 offset:%13\n\tds_read_b64 %5, %9 offset:%13\n\tds_read_b64 %6, %10 offset:%13\n\tds_read_b64 %7, %11 offset:%13\n\t"
+                             "s_waitcnt lgkmcnt(0)"
+                             : "=&v"(v[t][0]), "=&v"(v[t][1]), "=&v"(v[t][2]), "=&v"(v[t][3]), "=&v"(v[t + 1][0]), "=&v"(v[t + 1][1]), "=&v"(v[t + 1][2]), "=&v"(v[t + 1][3])
+                             : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(t * 16 * RV), "n"((t + 1) * 16 * RV) : "memory");
         }
-#pragma unroll
-        for (int t = 0; t < D / 16; ++t)
-#pragma unroll
-            for (int i = 0; i < H; ++i) vw[i][t] = load_once(a[i] + (size_t)t * 16 * p.page_size * E);
-    }
-
-    __device__ __forceinline__ void first_product(const bf16x8 (&q)[D / 32], f32x4 (&z)[H][NS]) const
-    {
-#pragma unroll
-        for (int i = 0; i < H; ++i)
-#pragma unroll
-            for (int j = 0; j < NS; ++j) {
-                z[i][j] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int k = 0; k < KL; ++k) {
-                    const uint4 u = kw[i][j][k];
-                    if (F8) {
-                        z[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(make_uint2(u.x, u.y)), q[2 * k], z[i][j], 0, 0, 0);
-                        z[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(make_uint2(u.z, u.w)), q[2 * k + 1], z[i][j], 0, 0, 0);
-                    } else {
-                        z[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u), q[k], z[i][j], 0, 0, 0);
-                    }
-                }
-            }
-    }
-
-    // Weights and second product.  pos: position of the lane's row (-1: no row); pmin, pmax: least and greatest position of the
-    // tile's rows.
-    __device__ __forceinline__ void second_product(const AttnParams &p, int t0, f32x4 (&z)[H][NS], int pos, int pmin, int pmax, RowState<D> &s)
-    {
-        float x[H][LT];
-#pragma unroll
-        for (int i = 0; i < H; ++i)
-#pragma unroll
-            for (int j = 0; j < LT; ++j) x[i][j] = z[i][j / 4][j % 4] * p.scale2;
-        // Tokens that not every row of the tile sees.  A token that none sees may hold anything, also what is no number: its
-        // value is replaced by zero, since zero times it would not be.
-        const bool in_window = p.window == 0 || t0 > pmax - p.window || t0 + kBlock <= p.sinks;
-        if (!(t0 + kBlock - 1 <= pmin && in_window && __all(there == (1u << H) - 1u))) {
-#pragma unroll
-            for (int i = 0; i < H; ++i) {
-                const int vt = run_token(t0, i);
-                const int ok = there >> i & 1u;
-#pragma unroll
-                for (int j = 0; j < LT; ++j) x[i][j] = ok & seen(p, vt + j, pos, pos) ? x[i][j] : -INFINITY;
-                uint32_t mask[4];
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    mask[w] = 0u;
-#pragma unroll
-                    for (int j = 0; j < 4 / E; ++j)
-                        mask[w] |= ok & seen(p, vt + w * (4 / E) + j, pmin, pmax) ? (F8 ? 0xffu << (8 * j) : 0xffffu << (16 * j)) : 0u;
-                }
-#pragma unroll
-                for (int t = 0; t < D / 16; ++t) {
-                    vw[i][t].x &= mask[0];
-                    vw[i][t].y &= mask[1];
-                    vw[i][t].z &= mask[2];
-                    vw[i][t].w &= mask[3];
-                }
-            }
-        }
-        float top = x[0][0];
-#pragma unroll
-        for (int i = 0; i < H; ++i)
-#pragma unroll
-            for (int j = 0; j < LT; ++j) top = fmaxf(top, x[i][j]);
-        const float m = fmaxf(s.m, row_max(top));
-        if (__any(m > s.m)) {
-            const float a = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s.m - m);
-            s.l *= a;
-#pragma unroll
-            for (int t = 0; t < D / 16; ++t) s.o[t] *= a;
-            s.m = m;
-        }
-        const float base = s.m == -INFINITY ? 0.0f : s.m;
-        // bf16 weights: half a step of 2^-8 each, of either sign, beside values that are bf16 themselves
-        bf16x8 w[H][LT / 8];
-#pragma unroll
-        for (int i = 0; i < H; ++i) {
-#pragma unroll
-            for (int j = 0; j < LT; ++j) {
-                x[i][j] = __builtin_amdgcn_exp2f(x[i][j] - base);
-                s.l += x[i][j];
-            }
-#pragma unroll
-            for (int j = 0; j < LT / 8; ++j)
-                w[i][j] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(x[i][8 * j], x[i][8 * j + 1]), pack_bf16(x[i][8 * j + 2], x[i][8 * j + 3]),
-                                                                 pack_bf16(x[i][8 * j + 4], x[i][8 * j + 5]), pack_bf16(x[i][8 * j + 6], x[i][8 * j + 7])));
-        }
-#pragma unroll
-        for (int t = 0; t < D / 16; ++t)
-#pragma unroll
-            for (int i = 0; i < H; ++i) {
-                const uint4 u = vw[i][t];
-                if (F8) {
-                    s.o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(make_uint2(u.x, u.y)), w[i][0], s.o[t], 0, 0, 0);
-                    s.o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(make_uint2(u.z, u.w)), w[i][LT / 8 - 1], s.o[t], 0, 0, 0);
-                } else {
-                    s.o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u), w[i][0], s.o[t], 0, 0, 0);
-                }
-            }
     }
 };
+
+// One block: products, softmax, and the loads four units ahead, of `next` where they are past this block's (LAST: there is no next one).
+// pos: position of the lane's row (-1: no row); pmin, pmax: least and greatest position of the tile's rows.
+template <int D, bool F8, bool LAST>
+__device__ __forceinline__ void row_block(const AttnParams &p, int h, const Step<D, F8> &b, Step<D, F8> &next, int next_t0, typename Step<D, F8>::Pages &pages,
+                                          const int32_t *row, int t2, u32x4 *const (&place)[4],
+                                          const bf16x8 (&q)[D / 32], int pos, int pmin, int pmax, RowState<D> &s)
+{
+    typedef Step<D, F8> S;
+    constexpr int NU = S::NU, NG = S::NG, NT = S::NT;
+    const int t0 = b.t0, quad = lane_id() >> 4;
+    const auto ahead = [&](int n) {                // the loads behind unit n
+        if (n + 4 < 2 * NU) b.load(p, h, n + 4, place[n % 4]);
+        else if (!LAST) next.load(p, h, n + 4 - 2 * NU, place[n % 4]);
+    };
+    f32x4 z[4];
+    const auto first_products = [&](auto unit) {
+        constexpr int n = decltype(unit)::value;
+        wait_loads<S::NL * (LAST && 2 * NU - 1 - n < 3 ? 2 * NU - 1 - n : 3)>();
+        if (n == 2 * NU - 4 && !LAST) next.begin(p, h, next_t0, pages);
+        u32x4 k[NG][S::KL];
+        S::keys(place[n % 4], k);
+        ahead(n);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            f32x4 &c = z[n * NG + g];
+            c = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int j = 0; j < S::KL; ++j) {
+                const u32x4 u = k[g][j];
+                if (F8) {
+                    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(make_uint2(u.x, u.y)), q[2 * j], c, 0, 0, 0);
+                    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(make_uint2(u.z, u.w)), q[2 * j + 1], c, 0, 0, 0);
+                } else {
+                    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u), q[j], c, 0, 0, 0);
+                }
+            }
+        }
+    };
+    first_products(std::integral_constant<int, 0>());
+    first_products(std::integral_constant<int, 1>());
+    if constexpr (NU == 4) {
+        first_products(std::integral_constant<int, 2>());
+        first_products(std::integral_constant<int, 3>());
+    }
+
+    typename S::Pages after;
+    if (!LAST) after = S::fetch_pages(p, row, t2);
+    // Tokens that not every row of the tile sees.  A token that none sees may hold anything, also what is no number: its
+    // value is replaced by zero, since zero times it would not be.
+    const bool in_window = p.window == 0 || t0 > pmax - p.window || t0 + kBlock <= p.sinks;
+    const bool partly = !(t0 + kBlock - 1 <= pmin && in_window && b.there == 15u);
+    float x[4][4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[g][j] = z[g][j] * p.scale2;
+    typename S::Four mask[4];
+    if (partly) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int ok = b.there >> g & 1u, vt = t0 + 16 * g + 4 * quad;
+            unsigned bits[2] = {0u, 0u};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[g][j] = ok & seen(p, vt + j, pos, pos) ? x[g][j] : -INFINITY;
+                bits[F8 ? 0 : j / 2] |= ok & seen(p, vt + j, pmin, pmax) ? (F8 ? 0xffu << (8 * j) : 0xffffu << (16 * (j & 1))) : 0u;
+            }
+            if constexpr (F8) mask[g] = bits[0];
+            else mask[g] = {bits[0], bits[1]};
+        }
+    }
+    float top = x[0][0];
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, x[g][j]);
+    const float m = fmaxf(s.m, row_max(top));
+    if (__any(m > s.m)) {
+        const float a = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s.m - m);
+        s.l *= a;
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) s.o[t] *= a;
+        s.m = m;
+    }
+    const float base = s.m == -INFINITY ? 0.0f : s.m;
+    // bf16 weights: half a step of 2^-8 each, of either sign, beside values that are bf16 themselves
+    bf16x8 w[2];
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[g][j] = __builtin_amdgcn_exp2f(x[g][j] - base);
+            s.l += x[g][j];
+        }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        w[i] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(x[2 * i][0], x[2 * i][1]), pack_bf16(x[2 * i][2], x[2 * i][3]),
+                                                     pack_bf16(x[2 * i + 1][0], x[2 * i + 1][1]), pack_bf16(x[2 * i + 1][2], x[2 * i + 1][3])));
+
+    const auto second_products = [&](auto unit) {
+        constexpr int n = decltype(unit)::value;
+        wait_loads<S::NL * (LAST && 2 * NU - 1 - n < 3 ? 2 * NU - 1 - n : 3)>();
+        if (n == 2 * NU - 4 && !LAST) next.begin(p, h, next_t0, pages);
+        typename S::Four v[NT][4];
+        S::values_of(place[n % 4], v);
+        ahead(n);
+        if (partly) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) v[t][g] &= mask[g];
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            f32x4 &c = s.o[(n - NU) * NT + t];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                bf16x8 u;
+                if constexpr (F8) u = widen8(make_uint2(v[t][2 * i], v[t][2 * i + 1]));
+                else u = __builtin_bit_cast(bf16x8, u32x4{v[t][2 * i].x, v[t][2 * i].y, v[t][2 * i + 1].x, v[t][2 * i + 1].y});
+                c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, w[i], c, 0, 0, 0);
+            }
+        }
+    };
+    second_products(std::integral_constant<int, NU>());
+    second_products(std::integral_constant<int, NU + 1>());
+    if constexpr (NU == 4) {
+        second_products(std::integral_constant<int, NU + 2>());
+        second_products(std::integral_constant<int, NU + 3>());
+    }
+    if (!LAST) pages = after;
+}
 
 // The rows' queries as operand: lane l holds row l % 16; channels in the order in which a lane's key loads bring them.
 template <int D, bool F8>
@@ -436,7 +537,7 @@ struct RowsShared {
 };
 // part(k): 16 rows of D floats of LDS.
 template <int D, bool F8, typename Parts>
-__device__ __forceinline__ void rows_of(const AttnParams &p, unsigned x, int h, RowsShared &sh, const Parts &part_of)
+__device__ __forceinline__ void rows_of(const AttnParams &p, unsigned x, int h, RowsShared &sh, u32x4 *const (&units)[4], const Parts &part_of)
 {
     typedef Step<D, F8> S;
     constexpr unsigned kNone = 0xffffffffu;
@@ -453,6 +554,8 @@ __device__ __forceinline__ void rows_of(const AttnParams &p, unsigned x, int h, 
     if (lane < 2) rec[2 * wv + lane] = kNone;
     const unsigned quarter = (length + kAttnWaves - 1) / kAttnWaves;
     const unsigned wfrom = min(from + wv * quarter, to), wto = min(wfrom + quarter, to);
+    RowState<D> s, left;           // left: of the first tile, where its part goes to LDS in the end (until then loads go there)
+    int last = 0;                  // whether s at the end is such a part too
     for (unsigned at = wfrom; at < wto;) {
         const Place f = place_of(p, line, at);
         const unsigned i0 = at - f.begin, i1 = min(f.count, wto - f.begin);
@@ -465,7 +568,6 @@ __device__ __forceinline__ void rows_of(const AttnParams &p, unsigned x, int h, 
         const int pmin = max(f.seq - f.n + token_of(p, f.tile * kRows), 0), pmax = f.seq - f.n + token_of(p, min(f.tile * kRows + kRows, rows) - 1);
         bf16x8 q[D / 32];
         load_queries<D, F8>(p.q + (size_t)(f.first + tok) * p.q_stride + (size_t)head * D, real, q);
-        RowState<D> s;
         s.m = -INFINITY;
         s.l = 0.0f;
 #pragma unroll
@@ -477,46 +579,43 @@ __device__ __forceinline__ void rows_of(const AttnParams &p, unsigned x, int h, 
         const int32_t *row = p.table + (size_t)f.b * p.max_pages;
         const auto token = [&](int j) { return blocks.at(min(j, j1 - 1)) * kBlock; };
         if (j0 < j1) {
-            S step;
-            int t0 = token(j0);
-            step.fetch_pages(p, row, t0);
-            step.fetch_keys(p, h, t0);
-            step.fetch_values(p, h, t0);
-            S next;
-            next.fetch_pages(p, row, token(j0 + 1));
-            f32x4 z[S::H][S::NS];
-            for (int j = j0; j + 1 < j1; ++j) {
-                // The next keys as soon as the first product has used these, the next values behind the second; page numbers a
-                // block earlier, in front of them (loads come back in the order of their issue).
-                const int t1 = token(j + 1);
-                step.first_product(q, z);
+            S b, next;
+            typename S::Pages pages = S::fetch_pages(p, row, token(j0));
+            b.begin(p, h, token(j0), pages);
+            pages = S::fetch_pages(p, row, token(j0 + 1));
+            // the queries are there: waited for behind the loads into LDS, they would be waited for with all of those
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_waitcnt(0x0f70);     // vmcnt(0)
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < S::H; ++i) {
-                    step.kid[i] = next.kid[i];
-                    step.vid[i] = next.vid[i];
-                }
-                next.fetch_pages(p, row, token(j + 2));
-                step.fetch_keys(p, h, t1);
-                step.second_product(p, t0, z, pos, pmin, pmax, s);
-                step.fetch_values(p, h, t1);
-                t0 = t1;
+            for (int n = 0; n < 4; ++n) b.load(p, h, n, units[n]);
+            for (int j = j0; j + 1 < j1; ++j) {
+                row_block<D, F8, false>(p, h, b, next, token(j + 1), pages, row, token(j + 2), units, q, pos, pmin, pmax, s);
+                b = next;
             }
-            step.first_product(q, z);
-            step.second_product(p, t0, z, pos, pmin, pmax, s);
+            row_block<D, F8, true>(p, h, b, next, 0, pages, row, 0, units, q, pos, pmin, pmax, s);
         }
         s.l = row_sum(s.l);
         if (i0 == 0 && i1 == f.count) {
             if (real) finish_row<D>(p, f.first + tok, head, behind_prefix(p, f.seq - f.n), (lane >> 4) * 4, 16, s.m, s.l, s.o);
         } else {
-            const int k = 2 * wv + (at == wto && i0 == 0 ? 1 : 0);      // the wave's last tile, or its first
-            if (lane < kRows) {
-                sm[k][lane] = s.m;
-                sl[k][lane] = s.l;
-            }
-            if (lane == 0) rec[k] = f.begin;
-#pragma unroll
-            for (int t = 0; t < D / 16; ++t) place(k, lane & 15, t * 16 + (lane >> 4) * 4) = s.o[t];
+            last = at == wto && i0 == 0;            // the wave's last tile, or its first
+            if (lane == 0) rec[2 * wv + last] = f.begin;
+            if (!last) left = s;
         }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int k = 2 * wv + i;
+        if (rec[k] == kNone) continue;
+        const RowState<D> &part = i == 0 ? left : s;
+        if (lane < kRows) {
+            sm[k][lane] = part.m;
+            sl[k][lane] = part.l;
+        }
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) place(k, lane & 15, t * 16 + (lane >> 4) * 4) = part.o[t];
     }
     __syncthreads();
     // The parts in LDS, in the order of the line: those of one tile follow one another.  16 threads per row, D / 16 channels each.
@@ -635,6 +734,7 @@ __device__ __forceinline__ void join_rows(const AttnParams &p, unsigned cut_inde
 // each) and about as many VALU cycles for 32 weights per lane; two workgroups a CU, so that one's softmax stands beside the
 // other's products.
 constexpr int kWaveRows = 32;
+constexpr int kLdsAlign = 16384, kBuffer = kLdsAlign / 16;      // bytes and 16-byte pieces of each of the four buffers in LDS
 constexpr int kMinChunk = 8;                // blocks: a part of a tile's context is not made shorter
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -856,8 +956,8 @@ __device__ __forceinline__ void blocks_ready()
 // prefix: the rows are those of the whole batch, whatever request they belong to, and the context is the shared prefix's whole blocks,
 // which all of them see; every row's part is left in the workspace.
 template <int D, bool F8>
-__device__ __forceinline__ void tile_of(const AttnParams &p, bool prefix, int x, int h, u32x4 (&kbuf0)[kBlock * D / 8], u32x4 (&vbuf0)[kBlock * D / 8],
-                                        u32x4 (&kbuf1)[kBlock * D / 8], u32x4 (&vbuf1)[kBlock * D / 8])
+__device__ __forceinline__ void tile_of(const AttnParams &p, bool prefix, int x, int h, u32x4 (&kbuf0)[kBuffer], u32x4 (&vbuf0)[kBuffer],
+                                        u32x4 (&kbuf1)[kBuffer], u32x4 (&vbuf1)[kBuffer])
 {
     typedef BlockLoad<D, F8> B;
     constexpr int NQ = D / 16, NV = D / 32, kAhead = 4;     // fragments are read from LDS four products ahead
@@ -1078,17 +1178,15 @@ __device__ __forceinline__ void tile_of(const AttnParams &p, bool prefix, int x,
 // One launch for all of a call: the prefix's tiles, the tiles of requests of many rows, and the line of the others, whose reading of the
 // cache stands beside the tiles' products (three launches one after the other: prefix of 8011, 100 requests, 8-bit cache 94 us,
 // this 82; 40 mixed requests of D = 64 86 us, this 72).
-constexpr int kLdsAlign = 16384;
 template <int D, bool F8, bool TILES>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_kernel(AttnParams p)
 {
     // Loads into LDS reach its first 64 KiB, so these four arrays have to come first.  They are aligned to more than the rest of the LDS
-    // takes: if anything stood in front of one, the kernel's LDS would be larger by a whole kLdsAlign, which the build looks for (with
-    // D = 64 all of the LDS is less than 64 KiB).  They are four, since which of two buffers is meant has to be known when this is compiled, for a read of one not to wait for loads
+    // takes: if anything stood in front of one, the kernel's LDS would be larger by a whole kLdsAlign, which the build looks for.  They are four, since which of two buffers is meant has to be known when this is compiled, for a read of one not to wait for loads
     // into the other.
-    __shared__ __align__(D == 128 ? kLdsAlign : 1024) u32x4 kbuf0[kBlock * D / 8], vbuf0[kBlock * D / 8], kbuf1[kBlock * D / 8], vbuf1[kBlock * D / 8];
+    __shared__ __align__(kLdsAlign) u32x4 kbuf0[kBuffer], vbuf0[kBuffer], kbuf1[kBuffer], vbuf1[kBuffer];
     __shared__ RowsShared rows;
-    static_assert(4 * sizeof kbuf0 <= 65536 && 2 * kRows * D * 4 == sizeof kbuf0 && sizeof rows < kLdsAlign, "LDS");
+    static_assert(4 * sizeof kbuf0 == 65536 && 2 * kRows * D * 4 <= sizeof kbuf0 && kBlock * D * 2 <= sizeof kbuf0 && kAttnWaves * Step<D, F8>::kUnit <= sizeof kbuf0 && sizeof rows < kLdsAlign, "LDS");
     unsigned x = blockIdx.x;
     if (TILES) {
         const bool prefix = x < p.prefix_groups;
@@ -1099,7 +1197,9 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_kernel(AttnParams p)
         }
         x -= p.tile_groups;
     }
-    rows_of<D, F8>(p, x / p.KVH, x % p.KVH, rows, [&](int k) {
+    const int wave = __builtin_amdgcn_readfirstlane(wave_id()) * (Step<D, F8>::kUnit / 16);
+    u32x4 *const units[4] = {kbuf0 + wave, vbuf0 + wave, kbuf1 + wave, vbuf1 + wave};
+    rows_of<D, F8>(p, x / p.KVH, x % p.KVH, rows, units, [&](int k) {
         float *const half = reinterpret_cast<float *>(k < 4 ? (k < 2 ? kbuf0 : vbuf0) : (k < 6 ? kbuf1 : vbuf1));
         return half + (k & 1) * (kRows * D);
     });
