@@ -48,6 +48,8 @@ struct AttnParams {
     float *prefix_o, *prefix_ml;        // the parts of all rows,
     float *own_o, *own_ml;              // and what the rows behind the prefix see of their own sequences
     unsigned prefix_groups, tile_groups; // workgroups of the prefix's tiles and of the others
+    unsigned turns;                     // their order: attn_kernel
+    int tiles_first;
 };
 
 // Page (index in a row of the table) of the 16 tokens from 16 * group on: group / (page_size / 16), by multiplication.
@@ -1178,6 +1180,12 @@ __device__ __forceinline__ void tile_of(const AttnParams &p, bool prefix, int x,
 // One launch for all of a call: the prefix's tiles, the tiles of requests of many rows, and the line of the others, whose reading of the
 // cache stands beside the tiles' products (three launches one after the other: prefix of 8011, 100 requests, 8-bit cache 94 us,
 // this 82; 40 mixed requests of D = 64 86 us, this 72).
+// Behind a prefix, both kinds are large, and as long as there are workgroups of both they take turns of one to a CU, so that a CU has one
+// of each: 256 requests of 1000 tokens behind 30000: 193 us with all tiles in front, 176 in turns.  Where a prefix's tile has at least
+// kLongPart blocks it goes first (256 requests of 2000 behind 8000, 15 blocks: 225 us, the line first 232; behind 24000: 232 and 269),
+// else the line (64 of 1500 behind 16000, 8 blocks: 123 us, tiles first 130; 256 of 1096 behind 3000, 6 blocks: 136 and 156).
+// Without a prefix all tiles go first (40 mixed requests: 71.3 us, in turns 74.4).
+constexpr int kTurn = 256, kLongPart = 12;
 template <int D, bool F8, bool TILES>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_kernel(AttnParams p)
 {
@@ -1189,13 +1197,23 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_kernel(AttnParams p)
     static_assert(4 * sizeof kbuf0 == 65536 && 2 * kRows * D * 4 <= sizeof kbuf0 && kBlock * D * 2 <= sizeof kbuf0 && kAttnWaves * Step<D, F8>::kUnit <= sizeof kbuf0 && sizeof rows < kLdsAlign, "LDS");
     unsigned x = blockIdx.x;
     if (TILES) {
-        const bool prefix = x < p.prefix_groups;
-        if (!prefix) x -= p.prefix_groups;
-        if (prefix || x < p.tile_groups) {
+        const unsigned tiles = p.prefix_groups + p.tile_groups;
+        bool tile;
+        if (x < p.turns * 2 * kTurn) {
+            const unsigned turn = x / (2 * kTurn), at = x % (2 * kTurn);
+            tile = (at < kTurn) == (p.tiles_first != 0);
+            x = turn * kTurn + at % kTurn;
+        } else {
+            x -= p.turns * kTurn;
+            tile = x < tiles;
+            if (!tile) x -= tiles - p.turns * kTurn;
+        }
+        if (tile) {
+            const bool prefix = x < p.prefix_groups;
+            if (!prefix) x -= p.prefix_groups;
             tile_of<D, F8>(p, prefix, x / p.KVH, x % p.KVH, kbuf0, vbuf0, kbuf1, vbuf1);
             return;
         }
-        x -= p.tile_groups;
     }
     const int wave = __builtin_amdgcn_readfirstlane(wave_id()) * (Step<D, F8>::kUnit / 16);
     u32x4 *const units[4] = {kbuf0 + wave, vbuf0 + wave, kbuf1 + wave, vbuf1 + wave};
@@ -1368,6 +1386,8 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
     p.prefix_groups = p.prefix_blocks > 0 ? (unsigned)KVH * w.prefix_tiles * w.prefix_splits : 0u;
     p.tile_groups = wide ? KVH * (tiles + w.wide_parts) : 0u;
     const bool any_tiles = p.prefix_groups + p.tile_groups > 0;
+    p.turns = p.prefix_groups > 0 ? std::min(p.prefix_groups + p.tile_groups, (unsigned)(KVH * w.parts)) / kTurn : 0u;
+    p.tiles_first = p.prefix_groups > 0 && p.prefix_blocks / w.prefix_splits >= kLongPart;
     auto kernel = D == 128 ? (f8 ? (any_tiles ? attn_kernel<128, true, true> : attn_kernel<128, true, false>)
                                  : (any_tiles ? attn_kernel<128, false, true> : attn_kernel<128, false, false>))
                            : (f8 ? (any_tiles ? attn_kernel<64, true, true> : attn_kernel<64, true, false>)

@@ -233,6 +233,36 @@ def test_prefix_on_any_workspace():
         assert torch.equal(c.run(workspace=ws)[:c.rows], want[:c.rows])
 
 
+@pytest.mark.parametrize("prefix,fp8", [(8229, False), (24600, False), (24600, True)])
+def test_prefixes_long_enough_that_tiles_and_requests_take_turns(prefix, fp8):
+    B, QH, KVH, D, ps, own = 128, 16, 4, 64, 64, 3
+    G, common, dt = QH // KVH, prefix // ps, torch.float8_e4m3fn if fp8 else torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(31)
+    pages = common + B * own
+    kc, vc = (torch.randn(shape, generator=g, device="cuda").to(dt) for shape in ((pages, KVH, ps, D), (pages, KVH, D, ps)))
+    order = torch.randperm(pages, generator=g, device="cuda").to(torch.int32)
+    table = torch.cat([order[:common].expand(B, common), order[common:].view(B, own)], 1).contiguous()
+    # what every request has of the page that the prefix ends in is the same
+    for cache, at in ((kc, (slice(None), slice(0, prefix % ps))), (vc, (slice(None), slice(None), slice(0, prefix % ps)))):
+        raw = cache.view(torch.uint8) if fp8 else cache
+        raw[(table[:, common].long(),) + at] = raw[(table[0, common].long(),) + at].clone()
+    seq = [prefix + 1 + 7 * b % 120 for b in range(B)]
+    q = torch.randn(B, QH, D, generator=g, device="cuda").to(torch.bfloat16)
+    out = L.lynx_attention_prefix(q, kc, vc, table, i32(list(range(B + 1))), i32(seq), 1, table[0, :-(-prefix // ps)].contiguous(), prefix)
+    for b in range(0, B, 5):
+        ids = table[b].long()
+        k = kc[ids].double().transpose(0, 1).reshape(KVH, -1, D)[:, :seq[b]].contiguous()
+        v = vc[ids].double().permute(1, 0, 3, 2).reshape(KVH, -1, D)[:, :seq[b]].contiguous()
+        qq = q[b].double().view(KVH, G, D)
+        for h in range(KVH):
+            w = torch.softmax(qq[h] @ k[h].t().contiguous() * D ** -0.5, 1)
+            want, size = w @ v[h], w @ v[h].abs()
+            # weights and result are rounded to bf16, 2^-8 of the value each; scores are 80 fp32 roundings off at most, as in the oracle's bound
+            shake = (D + 16) * 2.0 ** -24 * float((qq[h].abs() @ k[h].abs().t().contiguous()).max()) * D ** -0.5
+            tol = 2.0 ** -8 * (size + want.abs()) * 1.02 + 2 * shake * size
+            assert bool(((out[b, h * G:(h + 1) * G].double() - want).abs() <= tol).all()), (b, h)
+
+
 # ---- all of it together ------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("fp8", [False, True])
