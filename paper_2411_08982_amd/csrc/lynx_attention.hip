@@ -1271,39 +1271,61 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p, u
     }
 }
 
-// Rows behind the shared prefix: joins the prefix's parts and the row's own.  D / 4 lanes to a row, rows in the order of out.
+// What is left behind a call with a shared prefix: a row behind the prefix is joined from the prefix's parts and its own, and where the
+// row's tile of 16 is cut, from that tile's parts, which join_rows would join first (its launch, of 5 us, is saved).  D / 4 lanes to a
+// row, rows in the order of out.
 template <int D>
 __global__ __launch_bounds__(kAttnThreads) void attn_finish_kernel(AttnParams p)
 {
     constexpr int L = D / 4, NG = kAttnThreads / L;
-    __shared__ int starts[LYNX_MAX_REQUESTS];
-    for (int b = threadIdx.x; b < p.B; b += kAttnThreads) starts[b] = p.q_start[b];
+    __shared__ Line line;
+    const unsigned total = lay_out(p, line), length = length_of(p, total);
     const int QH = p.KVH * p.G, row = blockIdx.x * NG + threadIdx.x / L, lane = threadIdx.x % L;
     const int t = row / QH, head = row % QH, h = head / p.G, r = t * p.G + head % p.G;
-    __syncthreads();
     if (t >= p.T) return;
     // the last request that begins at t or before
     int lo = 0, hi = p.B - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (starts[mid] <= t) lo = mid;
+        if ((int)(line.what[mid] >> 47) <= t) lo = mid;
         else hi = mid - 1;
     }
-    int first, n, seq;
-    request_of(p, lo, first, n, seq);
-    if (t < first || t >= first + n || !behind_prefix(p, seq - n)) return;
-    float m = p.own_ml[2 * (size_t)row], l = p.own_ml[2 * (size_t)row + 1];
-    f32x4 o[1] = {*reinterpret_cast<const f32x4 *>(p.own_o + (size_t)row * D + 4 * lane)};
-    size_t part = ((size_t)(r / kTileRows) * p.prefix_splits * p.KVH + h) * kTileRows + r % kTileRows;
-#pragma unroll 8
-    for (int i = 0; i < p.prefix_splits; ++i, part += (size_t)p.KVH * kTileRows) {
-        const float2 ml = *reinterpret_cast<const float2 *>(p.prefix_ml + 2 * part);
-        const f32x4 u = *reinterpret_cast<const f32x4 *>(p.prefix_o + part * D + 4 * lane);
-        const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.0f : top;
-        const float a = __builtin_amdgcn_exp2f(m - base), e = __builtin_amdgcn_exp2f(ml.x - base);
-        l = l * a + e * ml.y;
+    const unsigned long long what = line.what[lo];
+    const int first = (int)(what >> 47), n = (int)(what >> 30 & 0x1ffffu), seq = (int)(what & 0x3fffffffu);
+    if (t >= first + n) return;
+    const bool behind = behind_prefix(p, seq - n);
+    const int own_row = (t - first) * p.G + head % p.G;
+    float m = -INFINITY, l = 0.0f;
+    f32x4 o[1] = {{0.0f, 0.0f, 0.0f, 0.0f}};
+    const auto join = [&](const float *ml, const float *values) {
+        const float2 w = *reinterpret_cast<const float2 *>(ml);
+        const f32x4 u = *reinterpret_cast<const f32x4 *>(values + 4 * lane);
+        const float top = fmaxf(m, w.x), base = top == -INFINITY ? 0.0f : top;
+        const float a = __builtin_amdgcn_exp2f(m - base), e = __builtin_amdgcn_exp2f(w.x - base);
+        l = l * a + e * w.y;
         o[0] = o[0] * a + u * e;
         m = top;
+    };
+    unsigned x = 0, last = 0, begin = 0;           // the lengths of the line that the row's tile lies in
+    if (n * p.G <= p.narrow && total > 0) {
+        const unsigned count = blocks_per_tile(p, n, seq);
+        begin = (lo > 0 ? line.ends[lo - 1] : 0u) + (unsigned)(own_row / kRows) * count;
+        x = begin / length;
+        last = (begin + count - 1) / length;
+    }
+    if (x < last) {
+        for (; x <= last; ++x) {
+            const size_t part = ((size_t)(2 * x + (begin >= x * length ? 1 : 0)) * p.KVH + h) * kRows + own_row % kRows;
+            join(p.part_ml + 2 * part, p.part_o + part * D);
+        }
+    } else {
+        if (!behind) return;
+        join(p.own_ml + 2 * (size_t)row, p.own_o + (size_t)row * D);
+    }
+    if (behind) {
+        size_t part = ((size_t)(r / kTileRows) * p.prefix_splits * p.KVH + h) * kTileRows + r % kTileRows;
+#pragma unroll 8
+        for (int i = 0; i < p.prefix_splits; ++i, part += (size_t)p.KVH * kTileRows) join(p.prefix_ml + 2 * part, p.prefix_o + part * D);
     }
     finish_row<D>(p, t, head, false, 4 * lane, 4, m, l, o);
 }
@@ -1396,7 +1418,7 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
     // a request's parts are w.parts / B on average: where they are many, a tile's rows go to four workgroups (one request of 9001 tokens:
     // 15 -> 4.4 us); else to one, since most workgroups have nothing to join (64 requests: 6.3 -> 4.9 us)
     const int slices = std::max(1, std::min(4, w.parts / (2 * B)));
-    const unsigned line_groups = (unsigned)(w.parts - 1) * KVH * slices, tile_joins = std::min(tiles, (unsigned)w.wide_parts) * KVH * kTileSlices;
+    const unsigned line_groups = p.prefix_blocks > 0 ? 0u : (unsigned)(w.parts - 1) * KVH * slices, tile_joins = std::min(tiles, (unsigned)w.wide_parts) * KVH * kTileSlices;
     if (line_groups + tile_joins > 0)
         hipLaunchKernelGGL((D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>), dim3(line_groups + tile_joins), threads, 0, st, p, line_groups, slices);
     if (p.prefix_blocks > 0)
