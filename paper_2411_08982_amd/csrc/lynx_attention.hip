@@ -1330,15 +1330,17 @@ __global__ __launch_bounds__(kAttnThreads) void attn_finish_kernel(AttnParams p)
     finish_row<D>(p, t, head, false, 4 * lane, 4, m, l, o);
 }
 
-// Requests of up to this many rows are read by tiles of 16 rows, others by tiles of 128.
-constexpr int kNarrowRows = 64;
+// Requests of up to this many rows are read by tiles of 16 rows, others by tiles of 128.  Two tiles of 16 read the cache twice (32 requests
+// of 4096 tokens, 8 key heads of 4 query heads: 20 rows 164 us, by one tile of 128 108 us; 64 rows 293 and 114; 64 requests with one
+// key head of 32: 58 and 44).  An 8-bit block, which a wide tile has to widen on its way into LDS, is better read twice, not more
+// often (100 requests of 250 to 2000: 32 rows 90 us, by a wide tile 116; 48 rows 128 and 117).
+inline int narrow_rows(bool f8) { return f8 ? 2 * kRows : kRows; }
 // What the workspace holds: rows of unfinished tiles with their maxima and sums.  A workgroup's length of the line leaves two tiles.
 // Tiles of 128 rows: a tile that is cut has more than `chunk` blocks, so its parts are fewer than twice blocks / chunk, all such
 // parts fewer than twice wide_parts, and such tiles at most wide_parts.
 // The prefix's tiles leave every row's parts, and the rows behind the prefix their own.
 struct AttnSpace {
     int parts, wide_parts, prefix_tiles, prefix_splits;
-    bool wide;
     size_t ml_off, wide_o_off, wide_ml_off, prefix_o_off, prefix_ml_off, own_o_off, own_ml_off, total;
 };
 static AttnSpace attention_space(int T, int G, int KVH, int D, int prefix_len)
@@ -1348,9 +1350,8 @@ static AttnSpace attention_space(int T, int G, int KVH, int D, int prefix_len)
     const size_t rows = (size_t)2 * w.parts * KVH * kRows;
     w.ml_off = align256(rows * D * 4);
     w.wide_o_off = w.ml_off + align256(rows * 8);
-    w.wide = (int64_t)T * G > kNarrowRows;
     w.wide_parts = w.parts;
-    const size_t wide_rows = w.wide ? (size_t)2 * w.wide_parts * KVH * kTileRows : 0;
+    const size_t wide_rows = (int64_t)T * G > kRows ? (size_t)2 * w.wide_parts * KVH * kTileRows : 0;
     w.wide_ml_off = w.wide_o_off + align256(wide_rows * D * 4);
     w.prefix_o_off = w.wide_ml_off + align256(wide_rows * 8);
     // as many parts of the prefix as fill the chip, of four blocks at least
@@ -1392,19 +1393,20 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
     if (((uintptr_t)workspace & 255) != 0) return fail(LYNX_ERR_INVALID_ARG, "%s: the workspace must start on 256 bytes", who);
     const int G = QH / KVH;
     const AttnSpace w = attention_space(T, G, KVH, D, prefix_len);
-    const bool wide = w.wide && (int64_t)max_new * G > kNarrowRows;
+    const int narrow = narrow_rows(cache_format == LYNX_CACHE_FP8);
+    const bool wide = (int64_t)T * G > narrow && (int64_t)max_new * G > narrow;
     char *const ws = (char *)workspace;
     AttnParams p = {q, k_cache, v_cache, block_table, q_start, seq_len, prefix_table, out, lse, q_stride, out_stride, B, T, KVH, G,
                     num_pages, max_pages, page_size, page_multiplier(page_size), reciprocal(G), reciprocal(w.parts), scale * k_scale * kLog2e, v_scale,
                     window < kMaxContext ? window : 0, sinks < kMaxContext ? sinks : kMaxContext,   // (a window that long hides nothing)
-                    w.parts, (float *)ws, (float *)(ws + w.ml_off), wide ? kNarrowRows : INT_MAX, w.wide_parts, (float *)(ws + w.wide_o_off),
+                    w.parts, (float *)ws, (float *)(ws + w.ml_off), wide ? narrow : INT_MAX, w.wide_parts, (float *)(ws + w.wide_o_off),
                     (float *)(ws + w.wide_ml_off), prefix_len / kBlock, w.prefix_splits, (float *)(ws + w.prefix_o_off), (float *)(ws + w.prefix_ml_off),
                     (float *)(ws + w.own_o_off), (float *)(ws + w.own_ml_off)};
     const bool f8 = cache_format == LYNX_CACHE_FP8;
     const dim3 threads(kAttnThreads);
     hipStream_t st = (hipStream_t)stream;
-    // tiles: at most the sum of ceil(rows / 128) over requests of more than kNarrowRows rows
-    const unsigned tiles = wide ? (unsigned)((int64_t)T * G / kTileRows + std::min<int64_t>(B, (int64_t)T * G / kNarrowRows)) : 0u;
+    // tiles: at most the sum of ceil(rows / 128) over requests of more than `narrow` rows
+    const unsigned tiles = wide ? (unsigned)((int64_t)T * G / kTileRows + std::min<int64_t>(B, (int64_t)T * G / narrow)) : 0u;
     p.prefix_groups = p.prefix_blocks > 0 ? (unsigned)KVH * w.prefix_tiles * w.prefix_splits : 0u;
     p.tile_groups = wide ? KVH * (tiles + w.wide_parts) : 0u;
     const bool any_tiles = p.prefix_groups + p.tile_groups > 0;
