@@ -41,6 +41,7 @@ struct AttnParams {
     int window, sinks;
     int parts;                          // parts that the contexts of all tiles together are cut into, per key head
     float *part_o, *part_ml;            // workspace: unfinished rows
+    struct Cut *cuts;                   // and which tiles are to be joined from them
     int narrow;                         // requests of more rows are left to the tiles of 128 rows
     int wide_parts;                     // tiles of 128 rows: parts that all their contexts are cut into, per key head
     float *wide_o, *wide_ml;
@@ -526,6 +527,12 @@ __device__ __forceinline__ void finish_row(const AttnParams &p, int t, int head,
     if (p.lse && c0 == 0) p.lse[row] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
+// Where the line is cut behind a workgroup's length: the tile that goes on there, if this is the first cut through it.
+struct alignas(16) Cut {
+    int first, n, seq, tile;
+    unsigned begin, count, length, mine;
+};
+
 // A length of the line of one key head per workgroup, a quarter of it per wave.  A wave goes through its quarter tile by tile.
 // A tile that lies in it whole is finished in its registers; of the first and the last, which in general do not, it leaves its part in
 // LDS, and when all waves are through, the parts of each tile are joined: to the finished rows, or to a part in the workspace if
@@ -552,6 +559,15 @@ __device__ __forceinline__ void rows_of(const AttnParams &p, unsigned x, int h, 
     const unsigned from = min(x * length, total), to = min(from + length, total);
     // (four channels of a row stand at their place xor the row: the lanes that write have one place of all 16 rows)
     const auto place = [&](int k, int row, int c) -> f32x4 & { return *reinterpret_cast<f32x4 *>(part_of(k) + row * D + (c / 4 ^ row) * 4); };
+    if (h == 0 && wv == kAttnWaves - 1) {
+        const unsigned cut = (x + 1) * length;
+        Cut c = {};
+        if (cut < total) {
+            const Place f = place_of(p, line, cut);
+            c = {f.first, f.n, f.seq, f.tile, f.begin, f.count, length, f.begin != cut && f.begin + length >= cut ? 1u : 0u};
+        }
+        if (lane == 0) p.cuts[x] = c;
+    }
     if (from >= to) return;
     if (lane < 2) rec[2 * wv + lane] = kNone;
     const unsigned quarter = (length + kAttnWaves - 1) / kAttnWaves;
@@ -672,13 +688,11 @@ template <int D>
 __device__ __forceinline__ void join_rows(const AttnParams &p, unsigned cut_index, int h, int slice, int slices)
 {
     constexpr int L = D / 4, NG = kAttnThreads / L;         // lanes of a group (4 channels each), groups
-    __shared__ Line line;
     __shared__ float sm[NG], sl[NG];
     __shared__ __align__(16) float4 so[NG][L];
-    const unsigned total = lay_out(p, line), length = length_of(p, total), cut = (cut_index + 1) * length;
-    if (cut >= total) return;
-    const Place f = place_of(p, line, cut);
-    if (f.begin == cut || f.begin + length < cut) return;          // between two tiles, or not the first cut of this one
+    const Cut f = p.cuts[cut_index];
+    if (!f.mine) return;
+    const unsigned length = f.length;
     const int here = min(f.n * p.G - f.tile * kRows, kRows);
     const int mine = (here - slice + slices - 1) / slices;        // of the tile's rows, those of this workgroup
     const int parts = (int)((f.begin + f.count - 1) / length) - (int)cut_index + 1;
@@ -1341,7 +1355,7 @@ inline int narrow_rows(bool f8) { return f8 ? 2 * kRows : kRows; }
 // The prefix's tiles leave every row's parts, and the rows behind the prefix their own.
 struct AttnSpace {
     int parts, wide_parts, prefix_tiles, prefix_splits;
-    size_t ml_off, wide_o_off, wide_ml_off, prefix_o_off, prefix_ml_off, own_o_off, own_ml_off, total;
+    size_t ml_off, cuts_off, wide_o_off, wide_ml_off, prefix_o_off, prefix_ml_off, own_o_off, own_ml_off, total;
 };
 static AttnSpace attention_space(int T, int G, int KVH, int D, int prefix_len)
 {
@@ -1349,7 +1363,8 @@ static AttnSpace attention_space(int T, int G, int KVH, int D, int prefix_len)
     w.parts = kWorkgroups / KVH > 0 ? kWorkgroups / KVH : 1;
     const size_t rows = (size_t)2 * w.parts * KVH * kRows;
     w.ml_off = align256(rows * D * 4);
-    w.wide_o_off = w.ml_off + align256(rows * 8);
+    w.cuts_off = w.ml_off + align256(rows * 8);
+    w.wide_o_off = w.cuts_off + align256((size_t)w.parts * sizeof(Cut));
     w.wide_parts = w.parts;
     const size_t wide_rows = (int64_t)T * G > kRows ? (size_t)2 * w.wide_parts * KVH * kTileRows : 0;
     w.wide_ml_off = w.wide_o_off + align256(wide_rows * D * 4);
@@ -1399,7 +1414,7 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
     AttnParams p = {q, k_cache, v_cache, block_table, q_start, seq_len, prefix_table, out, lse, q_stride, out_stride, B, T, KVH, G,
                     num_pages, max_pages, page_size, page_multiplier(page_size), reciprocal(G), reciprocal(w.parts), scale * k_scale * kLog2e, v_scale,
                     window < kMaxContext ? window : 0, sinks < kMaxContext ? sinks : kMaxContext,   // (a window that long hides nothing)
-                    w.parts, (float *)ws, (float *)(ws + w.ml_off), wide ? narrow : INT_MAX, w.wide_parts, (float *)(ws + w.wide_o_off),
+                    w.parts, (float *)ws, (float *)(ws + w.ml_off), (Cut *)(ws + w.cuts_off), wide ? narrow : INT_MAX, w.wide_parts, (float *)(ws + w.wide_o_off),
                     (float *)(ws + w.wide_ml_off), prefix_len / kBlock, w.prefix_splits, (float *)(ws + w.prefix_o_off), (float *)(ws + w.prefix_ml_off),
                     (float *)(ws + w.own_o_off), (float *)(ws + w.own_ml_off)};
     const bool f8 = cache_format == LYNX_CACHE_FP8;
