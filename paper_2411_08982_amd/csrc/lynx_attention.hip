@@ -98,10 +98,10 @@ __device__ __forceinline__ int seen(const AttnParams &p, int t, int pmin, int pm
 
 // How the work is cut.  The blocks of all tiles, one tile after the other, are one long line that is cut into equal lengths, one
 // for each workgroup that the chip holds at once: however ragged the contexts, all workgroups read the same amount (with whole tiles
-// dealt out, 64 requests of 500 to 12000 tokens took 100 us where the equal cut takes 71).  A tile that a cut goes through is
+// dealt out, 64 requests of 500 to 12000 tokens took 100 us where the equal cut took 71).  A tile that a cut goes through is
 // finished by attn_join_kernel.  Request lengths are on the device only: every workgroup sums them up for itself, one round trip
 // for the lengths (at most four requests a thread) and one scan.
-constexpr int kMinLength = 4;               // blocks: fewer are not worth a workgroup
+constexpr int kMinLength = 4;               // blocks of a workgroup at least, one a wave (16 requests of 300 tokens: 15.3 us, with 8 18.9; one of 9001: 18.3 and 17.1)
 constexpr int kMaxPerThread = LYNX_MAX_REQUESTS / kAttnThreads;
 struct Line {
     unsigned ends[LYNX_MAX_REQUESTS];       // where each request's blocks end on the line
@@ -537,7 +537,7 @@ struct alignas(16) Cut {
 // A tile that lies in it whole is finished in its registers; of the first and the last, which in general do not, it leaves its part in
 // LDS, and when all waves are through, the parts of each tile are joined: to the finished rows, or to a part in the workspace if
 // the tile goes on in another workgroup.  (With all four waves on one tile after the other, each with its round trips for lengths,
-// queries and page numbers, 256 requests with an 8-bit cache took 137 us where this takes 118.)
+// queries and page numbers, 256 requests with an 8-bit cache took 137 us where this took 118.)
 constexpr int kRecords = 2 * kAttnWaves;
 struct RowsShared {
     Line line;
@@ -559,7 +559,7 @@ __device__ __forceinline__ void rows_of(const AttnParams &p, unsigned x, int h, 
     const unsigned from = min(x * length, total), to = min(from + length, total);
     // (four channels of a row stand at their place xor the row: the lanes that write have one place of all 16 rows)
     const auto place = [&](int k, int row, int c) -> f32x4 & { return *reinterpret_cast<f32x4 *>(part_of(k) + row * D + (c / 4 ^ row) * 4); };
-    if (h == 0 && wv == kAttnWaves - 1) {
+    if (p.prefix_blocks == 0 && h == 0 && wv == kAttnWaves - 1) {         // (behind a prefix attn_finish_kernel finds them)
         const unsigned cut = (x + 1) * length;
         Cut c = {};
         if (cut < total) {
@@ -682,10 +682,9 @@ __device__ __forceinline__ void rows_of(const AttnParams &p, unsigned x, int h, 
 
 // Joins the parts of the tiles that are cut.  Workgroup x has the x-th cut of the line; where it is the first that goes through a
 // tile, it joins the tile.  Few rows with many parts each are the case that counts (one request alone: a few rows, dozens of
-// parts), so there a tile's rows are spread over several workgroups, and the parts of a row over what is left of the workgroup's D / 4-lane
-// groups, which meet in LDS.
+// parts), so the parts of a row are spread over what the rows leave of the workgroup's D / 4-lane groups, which meet in LDS.
 template <int D>
-__device__ __forceinline__ void join_rows(const AttnParams &p, unsigned cut_index, int h, int slice, int slices)
+__device__ __forceinline__ void join_rows(const AttnParams &p, unsigned cut_index, int h)
 {
     constexpr int L = D / 4, NG = kAttnThreads / L;         // lanes of a group (4 channels each), groups
     __shared__ float sm[NG], sl[NG];
@@ -694,21 +693,20 @@ __device__ __forceinline__ void join_rows(const AttnParams &p, unsigned cut_inde
     if (!f.mine) return;
     const unsigned length = f.length;
     const int here = min(f.n * p.G - f.tile * kRows, kRows);
-    const int mine = (here - slice + slices - 1) / slices;        // of the tile's rows, those of this workgroup
     const int parts = (int)((f.begin + f.count - 1) / length) - (int)cut_index + 1;
     const int grp = threadIdx.x / L, lane = threadIdx.x % L;
-    for (int done = 0; done < mine; done += NG) {
+    for (int done = 0; done < here; done += NG) {
         int width = 1;                                              // rows at a time: a power of two
-        while (width < mine - done && width < NG) width *= 2;
-        const int k = done + grp % width, sub = grp / width, orow = slice + k * slices;
-        const bool real = k < mine;
+        while (width < here - done && width < NG) width *= 2;
+        const int orow = done + grp % width, sub = grp / width;
+        const bool real = orow < here;
         float m = -INFINITY, l = 0.0f;
         f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
         for (int i = sub; i < parts; i += NG / width) {
             // the first part is the last of its workgroup unless the tile begins where the workgroup does
             const unsigned x = cut_index + i;
-            const size_t part = ((size_t)(2 * x + (f.begin >= x * length ? 1 : 0)) * p.KVH + h) * kRows + (real ? orow : slice);
+            const size_t part = ((size_t)(2 * x + (f.begin >= x * length ? 1 : 0)) * p.KVH + h) * kRows + (real ? orow : 0);
             const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * part);
             const f32x4 u = *reinterpret_cast<const f32x4 *>(p.part_o + part * D + 4 * lane);
             const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.0f : top;
@@ -751,7 +749,7 @@ __device__ __forceinline__ void join_rows(const AttnParams &p, unsigned cut_inde
 // other's products.
 constexpr int kWaveRows = 32;
 constexpr int kLdsAlign = 16384, kBuffer = kLdsAlign / 16;      // bytes and 16-byte pieces of each of the four buffers in LDS
-constexpr int kMinChunk = 8;                // blocks: a part of a tile's context is not made shorter
+constexpr int kMinChunk = 8;                // blocks: a part of a tile's context is not made shorter (one request of 3000 tokens, 100 of them new: 33.0 us, with 4 34.7, with 16 39.3)
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // The contexts of all tiles are cut into parts of at most `chunk` blocks, chunk following from the work of the whole batch, so that a
@@ -965,7 +963,7 @@ __device__ __forceinline__ void blocks_ready()
 }
 
 // Workgroups go round the eight XCDs, each with an L2 of its own, and the key heads go round fastest: the tiles of one head, which read
-// the same keys and values, meet in few L2s (prompt chunks with 8 key heads: 378 us with the heads slowest, 299 so).
+// the same keys and values, meet in few L2s (five prompt chunks with 8 key heads: 378 us with the heads slowest, 299 so).
 // A turn of the loop has the second product of one block and the first of the next, whose matrix instructions stand between the VALU
 // instructions of the softmax.  In LDS at a turn's start: its values and the next keys; on their way during it: the next values and
 // the keys after next.
@@ -1237,10 +1235,12 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_kernel(AttnParams p)
     });
 }
 
-// Joins the parts of the tiles of 128 rows that are cut: D / 4 lanes to a row.
-constexpr int kTileSlices = 4;
+// Joins the parts of the tiles of 128 rows that are cut: D / 4 lanes to a row, a tile's rows over 4 to 16 workgroups: as many as the chip
+// holds at once, since most find nothing to join where the batch is large (one request of 3000 tokens, 100 of them new: 39.4 us
+// with 1 workgroup a tile, 33.0 with 4, 29.5 with 16; 40 mixed requests: 72 us with 4, 80 with 16).
+constexpr int kJoinGroups = 2048;
 template <int D>
-__device__ __forceinline__ void join_tile(const AttnParams &p, int x, int h, int slice)
+__device__ __forceinline__ void join_tile(const AttnParams &p, int x, int h, int slice, int slices)
 {
     constexpr int L = D / 4, NG = kAttnThreads / L;
     __shared__ FindShared sh;
@@ -1249,7 +1249,7 @@ __device__ __forceinline__ void join_tile(const AttnParams &p, int x, int h, int
     int first, n, seq;
     request_of(p, f.b, first, n, seq);
     const int lane = threadIdx.x % L, here = min(n * p.G - f.tile * kTileRows, kTileRows);
-    for (int row = slice * (kTileRows / kTileSlices) + threadIdx.x / L; row < min((slice + 1) * (kTileRows / kTileSlices), here); row += NG) {
+    for (int row = slice * (kTileRows / slices) + threadIdx.x / L; row < min((slice + 1) * (kTileRows / slices), here); row += NG) {
         const size_t part = ((size_t)f.item * p.KVH + h) * kTileRows + row, step = (size_t)p.KVH * kTileRows;
         float m = -INFINITY, l = 0.0f;
         f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -1274,14 +1274,12 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p, u
 {
     unsigned x = blockIdx.x;
     if (x < line_groups) {
-        const int slice = x % slices;
-        x /= slices;
-        join_rows<D>(p, x / p.KVH, x % p.KVH, slice, slices);
+        join_rows<D>(p, x / p.KVH, x % p.KVH);
     } else {
         x -= line_groups;
-        const int slice = x % kTileSlices;
-        x /= kTileSlices;
-        join_tile<D>(p, x / p.KVH, x % p.KVH, slice);
+        const int slice = x % slices;
+        x /= slices;
+        join_tile<D>(p, x / p.KVH, x % p.KVH, slice, slices);
     }
 }
 
@@ -1432,10 +1430,9 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
                            : (f8 ? (any_tiles ? attn_kernel<64, true, true> : attn_kernel<64, true, false>)
                                  : (any_tiles ? attn_kernel<64, false, true> : attn_kernel<64, false, false>));
     hipLaunchKernelGGL(kernel, dim3(p.prefix_groups + p.tile_groups + (unsigned)KVH * w.parts), threads, 0, st, p);
-    // a request's parts are w.parts / B on average: where they are many, a tile's rows go to four workgroups (one request of 9001 tokens:
-    // 15 -> 4.4 us); else to one, since most workgroups have nothing to join (64 requests: 6.3 -> 4.9 us)
-    const int slices = std::max(1, std::min(4, w.parts / (2 * B)));
-    const unsigned line_groups = p.prefix_blocks > 0 ? 0u : (unsigned)(w.parts - 1) * KVH * slices, tile_joins = std::min(tiles, (unsigned)w.wide_parts) * KVH * kTileSlices;
+    const unsigned line_groups = p.prefix_blocks > 0 ? 0u : (unsigned)(w.parts - 1) * KVH, cut_tiles = std::min(tiles, (unsigned)w.wide_parts) * KVH;
+    const int slices = cut_tiles * 16 <= kJoinGroups ? 16 : cut_tiles * 8 <= kJoinGroups ? 8 : 4;
+    const unsigned tile_joins = cut_tiles * slices;
     if (line_groups + tile_joins > 0)
         hipLaunchKernelGGL((D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>), dim3(line_groups + tile_joins), threads, 0, st, p, line_groups, slices);
     if (p.prefix_blocks > 0)

@@ -9,7 +9,8 @@ namespace lynx {
 // page, returned page and token finds its request by bisection in the sums.  Nothing here is bound by bytes: one workgroup,
 // one thread per request, and what counts is the number of round trips.
 constexpr int kAssignThreads = LYNX_MAX_REQUESTS;
-constexpr int kTokensHere = 4096;       // more tokens are left to a launch of their own
+// More tokens are left to a launch of their own (64 requests: 2048 tokens 5.7 us here, 6.5 apart; 4096 7.3 and 6.7; 8192 10.6 and 6.6).
+constexpr int kTokensHere = 2048;
 
 struct AssignShared {
     int tok_end[LYNX_MAX_REQUESTS], take_end[LYNX_MAX_REQUESTS], back_end[LYNX_MAX_REQUESTS];
@@ -161,12 +162,14 @@ __global__ __launch_bounds__(kTokenThreads) void assign_tokens_kernel(AssignPara
 
 // ---- lynx_qk_norm_rope ------------------------------------------------------------------------------------------------
 // Workgroups of two kinds in one launch.  The first T have a token each, for its queries and keys: the angles are the same for all
-// heads and computed once, into LDS; a head row is held by D/8 lanes, 8 channels (16 bytes) each.  The others turn 64 tokens' values
+// heads and computed once, into LDS; a head row is held by D/8 lanes, 8 channels (16 bytes) each.  The others turn 32 tokens' values
 // of one key head over in LDS, since the cache has them transposed: where the tokens' slots follow one another, as a prompt's do, a
 // channel's run of 16 bytes is one store.  (Element by element 8001 tokens with 8 key heads took 70 us, with 16 of 16 heads 141.)
 constexpr int kRopeThreads = 256;
-constexpr int kTurnTokens = 64;
-constexpr int kFewTokens = 1024;        // up to so many tokens 16 at a time, for more workgroups
+// More at a time lose fewer runs at their borders, fewer have more workgroups (8 key heads; prompts that begin off a page: 8000 tokens
+// 35.4 us by 32, by 16 37.7, by 64 36.3; 256 tokens 5.2 by 32, 4.7 by 16, 6.4 by 64).
+constexpr int kTurnTokens = 32;
+constexpr int kFewTokens = 1024;        // up to so many tokens 16 at a time
 
 struct RopeParams {
     const uint16_t *q, *k, *v, *q_weight, *k_weight;
@@ -210,7 +213,7 @@ __device__ __forceinline__ uint2 pack8_fp8(const float (&x)[8], float scale)
     return make_uint2((unsigned)a, (unsigned)b);
 }
 
-// The values of up to 64 tokens of one key head into the cache.
+// The values of up to kTurnTokens tokens of one key head into the cache.
 template <int D, bool F8>
 __device__ __forceinline__ void write_values(const RopeParams &p, int t0, int h, uint8_t *lds, uint8_t (&list)[2][kTurnTokens])
 {
