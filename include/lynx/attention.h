@@ -8,7 +8,7 @@
  * hipGraph), LYNX_OK or a negative error with lynx_last_error(), nothing enqueued on error.  Inputs are assumed finite, except
  * that cache slots which no token occupies may hold anything.  No index array can cause an access out of bounds: tokens
  * whose page number lies outside [0, num_pages) are not written and not seen by any query, row ranges are clamped to [0, T], and
- * lengths to what a row of the block table can hold.
+ * lengths to what a row of the block table can hold; what rows of out hold that lie in several requests' ranges is not specified.
  *
  * A step: B requests, request b brings new_len[b] >= 0 new tokens behind the ctx_len[b] it has in the cache.  The T rows of q,
  * k, v, out, positions and slots hold the new tokens of request 0, then of request 1, and so on: request b's are rows
@@ -21,7 +21,8 @@
  * on 16 bytes.  FP8: value = code * k_scale or v_scale (host floats, > 0 and finite); bf16 caches take 1 for both.
  *
  * Limits: 1 <= B <= LYNX_MAX_REQUESTS, 0 <= T <= LYNX_MAX_STEP_TOKENS, D = 64 or 128, KVH divides QH, QH <= 1024,
- * QH / KVH <= 256, page_size <= LYNX_MAX_PAGE_SIZE, num_pages <= LYNX_MAX_PAGES, max_pages * page_size <= 2^29.
+ * QH / KVH <= 256, page_size <= LYNX_MAX_PAGE_SIZE, num_pages <= LYNX_MAX_PAGES, max_pages * page_size <= 2^29, and for the
+ * attention calls (B + T * QH / KVH / 16) * max_pages * page_size < 2^37.
  */
 #ifndef LYNX_ATTENTION_H
 #define LYNX_ATTENTION_H

@@ -1193,7 +1193,7 @@ __device__ __forceinline__ void tile_of(const AttnParams &p, bool prefix, int x,
 // cache stands beside the tiles' products (three launches one after the other: prefix of 8011, 100 requests, 8-bit cache 94 us,
 // this 82; 40 mixed requests of D = 64 86 us, this 72).
 // Behind a prefix, both kinds are large, and as long as there are workgroups of both they take turns of one to a CU, so that a CU has one
-// of each: 256 requests of 1000 tokens behind 30000: 193 us with all tiles in front, 176 in turns.  Where a prefix's tile has at least
+// of each: 256 requests of 10 to 2000 tokens behind 30000: 193 us with all tiles in front, 182 in turns.  Where a prefix's tile has at least
 // kLongPart blocks it goes first (256 requests of 2000 behind 8000, 15 blocks: 225 us, the line first 232; behind 24000: 232 and 269),
 // else the line (64 of 1500 behind 16000, 8 blocks: 123 us, tiles first 130; 256 of 1096 behind 3000, 6 blocks: 136 and 156).
 // Without a prefix all tiles go first (40 mixed requests: 71.3 us, in turns 74.4).
