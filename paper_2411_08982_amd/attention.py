@@ -183,8 +183,8 @@ def _attention(q, k_cache, v_cache, block_table, q_start, seq_len, max_new, scal
     need = attention_workspace_bytes(B, T, QH, KVH, D, prefix[1] if prefix else 0)
     if workspace is None:
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
-    elif workspace.get_device() != here or workspace.numel() * workspace.element_size() < need:
-        raise ValueError(f"workspace: on {workspace.device}, {workspace.numel() * workspace.element_size()} bytes; needed {need} on cuda:{here}")
+    elif workspace.get_device() != here or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
+        raise ValueError(f"workspace: on {workspace.device}, {workspace.numel() * workspace.element_size()} bytes; needed {need} contiguous on cuda:{here}")
     if prefix:
         call = lib().lynx_attention_prefix
         prefix = (_at(prefix[0], I32, -(-prefix[1] // page_size), here, "prefix_table"), prefix[1])

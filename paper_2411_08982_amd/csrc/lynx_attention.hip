@@ -12,6 +12,7 @@
 // Softmax in one pass: m = running maximum (of the scores times scale * log2 e), l = sum of 2^(s - m), O accumulates 2^(s - m) v; when
 // m grows, l and O are multiplied by 2^(m_old - m_new).  All in fp32.
 #include <algorithm>
+#include <cfloat>
 #include <climits>
 #include <type_traits>
 
@@ -1399,10 +1400,14 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
     if (most_tiles * (((int64_t)max_pages * page_size + kBlock - 1) / kBlock) >= (int64_t)1 << 31)
         return fail(LYNX_ERR_UNSUPPORTED, "%s: need (B + T * QH / KVH / 16) * max_pages * page_size < 2^37", who);
     if (!(scale > 0.0f) || scale > 3.0e38f) return fail(LYNX_ERR_INVALID_ARG, "%s: scale must be finite and > 0", who);
+    // (a masked score is -inf, which times a factor of 0 would be no number)
+    const float scale2 = scale * k_scale * kLog2e;
+    if (!(scale2 >= FLT_MIN) || scale2 > FLT_MAX) return fail(LYNX_ERR_INVALID_ARG, "%s: scale * k_scale leaves the range of a float", who);
     if (T == 0) return LYNX_OK;
     if (!block_table || !q_start || !seq_len || (prefix_len > 0 && !prefix_table) || !workspace)
         return fail(LYNX_ERR_INVALID_ARG, "%s: null pointer", who);
     if ((rc = check_rows(who, "q", q, q_stride, QH, D)) != LYNX_OK || (rc = check_rows(who, "out", out, out_stride, QH, D)) != LYNX_OK) return rc;
+    if (out == q) return fail(LYNX_ERR_INVALID_ARG, "%s: out must not be q", who);
     if (((uintptr_t)workspace & 255) != 0) return fail(LYNX_ERR_INVALID_ARG, "%s: the workspace must start on 256 bytes", who);
     const int G = QH / KVH;
     const AttnSpace w = attention_space(T, G, KVH, D, prefix_len);
@@ -1410,7 +1415,7 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
     const bool wide = (int64_t)T * G > narrow && (int64_t)max_new * G > narrow;
     char *const ws = (char *)workspace;
     AttnParams p = {q, k_cache, v_cache, block_table, q_start, seq_len, prefix_table, out, lse, q_stride, out_stride, B, T, KVH, G,
-                    num_pages, max_pages, page_size, page_multiplier(page_size), reciprocal(G), reciprocal(w.parts), scale * k_scale * kLog2e, v_scale,
+                    num_pages, max_pages, page_size, page_multiplier(page_size), reciprocal(G), reciprocal(w.parts), scale2, v_scale,
                     window < kMaxContext ? window : 0, sinks < kMaxContext ? sinks : kMaxContext,   // (a window that long hides nothing)
                     w.parts, (float *)ws, (float *)(ws + w.ml_off), (Cut *)(ws + w.cuts_off), wide ? narrow : INT_MAX, w.wide_parts, (float *)(ws + w.wide_o_off),
                     (float *)(ws + w.wide_ml_off), prefix_len / kBlock, w.prefix_splits, (float *)(ws + w.prefix_o_off), (float *)(ws + w.prefix_ml_off),

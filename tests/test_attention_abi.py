@@ -164,3 +164,11 @@ def test_block_buffers_lie_in_the_first_64_kib():
     assert check_code.check_attention_placement(notes % (65536 + 16383)) == 1
     with pytest.raises(RuntimeError, match="first 65536"):
         check_code.check_attention_placement(notes % (65536 + 16384))
+
+
+def test_scores_out_of_range_and_results_over_queries_are_refused():
+    other = ctypes.c_void_p(8192)
+    for kw in (dict(scale=1e-40), dict(scale=1e30, ks=1e30, fmt=1), dict(scale=1e-30, ks=1e-30, fmt=1)):
+        assert _attn(out=other, **kw) == -1 and b"scale * k_scale" in A.lib().lynx_last_error()
+        assert _attn(prefix=True, out=other, **kw) == -1
+    assert _attn(q=one, out=one) == -1 and b"out must not be q" in A.lib().lynx_last_error()

@@ -161,6 +161,56 @@ def test_row_ranges_that_overlap_beyond_all_bounds():
     assert bool((out == 7).all())
 
 
+def test_more_key_heads_than_the_line_has_workgroups():
+    Case([(0, 1), (70, 2), (130, 1), (0, 0)], 520, 520, 64, 16, seed=14).check()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("n", [1, 40])
+def test_pages_behind_four_gib(fp8, n):
+    # the last pages of caches whose offsets do not fit 32 bits: as in a small cache
+    c = Case([(150, n), (70, n)], 8, 2, 128, 64, fp8, seed=15)
+    want = c.run()
+    far = (5 << 30) // (2 * 64 * 128 * (1 if fp8 else 2))
+    small = c.kc.shape[0]
+    kc, vc = L.new_cache(far, 2, 64, 128, c.kc.dtype)
+    for big, cache in ((kc, c.kc), (vc, c.vc)):
+        big.view(torch.uint8)[far - small:].copy_(cache.view(torch.uint8))
+    c.kc, c.vc, c.table = kc, vc, [[p if p < 0 else p + far - small for p in row] for row in c.table]
+    assert torch.equal(c.run()[:c.rows], want[:c.rows])
+    if n == 1:
+        want = L.lynx_attention_prefix(c.q.cuda(), kc, vc, i32(c.table), i32(c.q_start), i32(c.seq), 1, i32([c.table[0][0]]), 64)
+        c.table[1][0] = 7                              # the prefix's own pages are not read
+        got = L.lynx_attention_prefix(c.q.cuda(), kc, vc, i32(c.table), i32(c.q_start), i32(c.seq), 1, i32([c.table[0][0]]), 64)
+        assert torch.equal(got[:c.rows], want[:c.rows])
+
+
+def test_two_graphs_on_one_workspace():
+    a, b = Case(MIXED, 8, 2, 128, 16, seed=16), Case([(200 + i, 1 + i % 2) for i in range(20)], 8, 2, 128, 16, seed=17, prefix=200)
+    wants = [c.run()[:c.rows] for c in (a, b)]
+    ws = torch.empty(max(L.attention_workspace_bytes(c.B, c.T, 8, 2, 128, c.prefix) for c in (a, b)), dtype=torch.uint8, device="cuda")
+    graphs, outs = [], []
+    for c in (a, b):
+        q, out = c.q.cuda(), torch.zeros(c.T, 8, 128, dtype=torch.bfloat16, device="cuda")
+        args = (q, c.kc, c.vc, i32(c.table), i32(c.q_start), i32(c.seq), c.max_new)
+        extra = (i32(c.prefix_table), c.prefix) if c.prefix else ()
+        call = L.lynx_attention_prefix if c.prefix else L.lynx_attention
+        call(*args, *extra, out=out, workspace=ws)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call(*args, *extra, out=out, workspace=ws)
+        graphs.append((g, args, extra))
+        outs.append(out)
+    for _ in range(4):
+        for (g, *_), out, want in zip(graphs, outs, wants):
+            out.zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out[:want.shape[0]], want)
+        ws.fill_(0x7F)
+
+
 def test_strided_rows():
     c = Case(MIXED, 6, 2, 64, 16, seed=10)
     out, _ = c.check()
@@ -341,3 +391,24 @@ def test_decode_steps_eager_and_as_a_graph(fp8):
                                          eager.a["q_start"].tolist(), eager.len.tolist(), D ** -0.5, k_scale=scales.get("k_scale", 1.0),
                                          v_scale=scales.get("v_scale", 1.0))
             assert bool(((eager.o[:n].cpu().double() - want[:n]).abs() <= tol[:n]).all())
+
+
+def test_the_binding_refuses_what_could_be_read_out_of_bounds():
+    c = Case([(20, 1), (3, 1)], 4, 2, 64, 16, seed=18)
+    q, need = c.q.cuda(), L.attention_workspace_bytes(c.B, c.T, 4, 2, 64)
+    args = (q, c.kc, c.vc, i32(c.table), i32(c.q_start), i32(c.seq), 1)
+    byte = torch.zeros(1, dtype=torch.uint8, device="cuda")
+    for ws in (byte.expand(need), torch.zeros(need - 1, dtype=torch.uint8, device="cuda"), torch.zeros(need, dtype=torch.uint8)):
+        with pytest.raises(ValueError, match="workspace"):
+            L.lynx_attention(*args, workspace=ws)
+    for i, bad in ((3, i32(c.table).t()), (4, i32(c.q_start)[:-1]), (5, i32(c.seq)[:1]), (5, i32(c.seq).long()), (1, c.kc.transpose(2, 3)), (0, q[:, :, :32])):
+        with pytest.raises((ValueError, TypeError)):
+            L.lynx_attention(*args[:i], bad, *args[i + 1:])
+    with pytest.raises(ValueError, match="out"):
+        L.lynx_attention(*args, out=torch.empty_like(q)[:-1])
+    with pytest.raises(ValueError, match="lse"):
+        L.lynx_attention(*args, lse=torch.empty(c.T * 4 - 1, device="cuda"))
+    with pytest.raises(L.LynxError, match="out must not be q"):
+        L.lynx_attention(*args, out=q)
+    with pytest.raises(ValueError, match="prefix_table"):
+        L.lynx_attention_prefix(*args, i32([0]), 17)
