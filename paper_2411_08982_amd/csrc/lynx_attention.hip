@@ -539,6 +539,8 @@ struct alignas(16) Cut {
 // LDS, and when all waves are through, the parts of each tile are joined: to the finished rows, or to a part in the workspace if
 // the tile goes on in another workgroup.  (With all four waves on one tile after the other, each with its round trips for lengths,
 // queries and page numbers, 256 requests with an 8-bit cache took 137 us where this took 118.)
+// Bound by HBM: 64 requests of 500 to 12000 tokens, 411 MB: 69 us, 6.0 TB/s; 256 with 657 MB of 8-bit cache: 118 us, 5.6 TB/s; a plain
+// read of such pages reaches 6.0, with the hint 6.6.  One request of 9001 tokens: 11.4 us, four dependent trips to memory.
 constexpr int kRecords = 2 * kAttnWaves;
 struct RowsShared {
     Line line;
@@ -681,7 +683,7 @@ __device__ __forceinline__ void rows_of(const AttnParams &p, unsigned x, int h, 
     }
 }
 
-// Joins the parts of the tiles that are cut.  Workgroup x has the x-th cut of the line; where it is the first that goes through a
+// Joins the parts of the tiles that are cut (4 to 5 us: a launch, two trips to memory).  Workgroup x has the x-th cut of the line; where it is the first that goes through a
 // tile, it joins the tile.  Few rows with many parts each are the case that counts (one request alone: a few rows, dozens of
 // parts), so the parts of a row are spread over what the rows leave of the workgroup's D / 4-lane groups, which meet in LDS.
 template <int D>
@@ -745,9 +747,10 @@ __device__ __forceinline__ void join_rows(const AttnParams &p, unsigned cut_inde
 // two buffers, and every fragment that a wave reads there serves 32 rows.  The same transposed products as above: a lane has row
 // l % 32, and a result fragment of S^T gives it 16 tokens of a block's half; the keys lie in LDS in such an order that they are two
 // runs of 8 consecutive tokens, the operand of the second product.
-// What bounds it: per block and wave 32 matrix instructions (1024 cycles), 32 KiB from LDS (four waves: 1024 cycles of its 128 bytes
-// each) and about as many VALU cycles for 32 weights per lane; two workgroups a CU, so that one's softmax stands beside the
-// other's products.
+// What bounds it: per block and wave 32 matrix instructions (1024 cycles; D = 64: 512), 32 KiB from LDS (four waves: 1024 cycles of its
+// 128 bytes each) and about 900 VALU cycles for 32 weights per lane, 512 of them exponentials; two workgroups a CU, so that one's
+// softmax stands beside the other's products.  Five prompt chunks of 700 to 2048 tokens, 236 GFLOP: 266 us, 890 TFLOP/s, matrix cores
+// and VALU 46 % busy each; with D = 64 it is the VALU's work (40 requests, 22 GFLOP: 72 us).
 constexpr int kWaveRows = 32;
 constexpr int kLdsAlign = 16384, kBuffer = kLdsAlign / 16;      // bytes and 16-byte pieces of each of the four buffers in LDS
 constexpr int kMinChunk = 8;                // blocks: a part of a tile's context is not made shorter (one request of 3000 tokens, 100 of them new: 33.0 us, with 4 34.7, with 16 39.3)
@@ -1286,7 +1289,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p, u
 
 // What is left behind a call with a shared prefix: a row behind the prefix is joined from the prefix's parts and its own, and where the
 // row's tile of 16 is cut, from that tile's parts, which join_rows would join first (its launch, of 5 us, is saved).  D / 4 lanes to a
-// row, rows in the order of out.
+// row, rows in the order of out.  Bound by the parts' bytes (256 requests, 8 parts, 33 MB: 10.8 us), with few rows by latency (12: 5.4).
 template <int D>
 __global__ __launch_bounds__(kAttnThreads) void attn_finish_kernel(AttnParams p)
 {
