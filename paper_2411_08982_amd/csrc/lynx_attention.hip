@@ -153,7 +153,7 @@ __device__ __forceinline__ unsigned lay_out(const AttnParams &p, Line &line)
         all += line.sum[w];
         work += line.work[w];
     }
-    if (work > 2147483648.0f) all = 0;
+    if (work > 4.0e9f) all = 0;
 #pragma unroll
     for (int i = 0; i < kMaxPerThread; ++i)
         if (i < per && b0 + i < p.B) line.ends[b0 + i] = before + sum[i];
@@ -1198,10 +1198,10 @@ __device__ __forceinline__ void tile_of(const AttnParams &p, bool prefix, int x,
 // this 82; 40 mixed requests of D = 64 86 us, this 72).
 // Behind a prefix, both kinds are large, and as long as there are workgroups of both they take turns of one to a CU, so that a CU has one
 // of each: 256 requests of 10 to 2000 tokens behind 30000: 193 us with all tiles in front, 182 in turns.  Where a prefix's tile has at least
-// kLongPart blocks it goes first (256 requests of 2000 behind 8000, 15 blocks: 225 us, the line first 232; behind 24000: 232 and 269),
-// else the line (64 of 1500 behind 16000, 8 blocks: 123 us, tiles first 130; 256 of 1096 behind 3000, 6 blocks: 136 and 156).
+// kLongPart blocks it goes first (256 requests behind 8000, 31 blocks: 70.5 us, the line first 75.1; behind 20000, 39 blocks: 134 and
+// 148), else the line (128 requests behind 8000, 15 blocks: 77.1 us, tiles first 87.5; 64 behind 16000, 15 blocks: 101 and 113).
 // Without a prefix all tiles go first (40 mixed requests: 71.3 us, in turns 74.4).
-constexpr int kTurn = 256, kLongPart = 12;
+constexpr int kTurn = 256, kLongPart = 24;
 template <int D, bool F8, bool TILES>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_kernel(AttnParams p)
 {
@@ -1371,10 +1371,22 @@ static AttnSpace attention_space(int T, int G, int KVH, int D, int prefix_len)
     const size_t wide_rows = (int64_t)T * G > kRows ? (size_t)2 * w.wide_parts * KVH * kTileRows : 0;
     w.wide_ml_off = w.wide_o_off + align256(wide_rows * D * 4);
     w.prefix_o_off = w.wide_ml_off + align256(wide_rows * 8);
-    // as many parts of the prefix as fill the chip, of four blocks at least
+    // As many parts of the prefix as fill the chip, of four blocks at least; or half as many, one to a CU beside the line of what the
+    // requests have of their own, where the parts would else have fewer than 32 blocks (each leaves its rows to be joined) and half the
+    // chip's workgroups come out nearly full.  512 requests behind 4000, 15 blocks: 277 us, half as many parts 228; 128 behind
+    // 16000, 15 blocks: 95 and 85; 64 behind 16000, 8 blocks: 121 and 101; 256 behind 16000, 31 blocks: 109 and 111, with 2000 tokens
+    // of their own 213 and 208; behind 30000, 58 blocks: 173 and 186.  100 requests of 2 to 5 tokens behind 8011, whose 88 tiles
+    // fill two thirds of one half: 78 and 94.
     const int blocks = prefix_len / kBlock;
     w.prefix_tiles = (int)(((int64_t)T * G + kTileRows - 1) / kTileRows);
-    w.prefix_splits = blocks > 0 && T > 0 ? std::max(1, std::min(kWorkgroups / (w.prefix_tiles * KVH), (blocks + 3) / 4)) : 0;
+    const int tiles = w.prefix_tiles * KVH;
+    w.prefix_splits = 0;
+    if (blocks > 0 && T > 0) {
+        int splits = std::max(1, kWorkgroups / tiles);
+        const int half = kWorkgroups / 2 / tiles;
+        if (blocks / splits < 32 && half * tiles * 8 >= kWorkgroups / 2 * 7) splits = half;
+        w.prefix_splits = std::min(splits, (blocks + 3) / 4);
+    }
     const size_t prefix_rows = (size_t)w.prefix_tiles * w.prefix_splits * KVH * kTileRows;
     w.prefix_ml_off = w.prefix_o_off + align256(prefix_rows * D * 4);
     w.own_o_off = w.prefix_ml_off + align256(prefix_rows * 8);
