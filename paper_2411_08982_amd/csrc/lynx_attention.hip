@@ -1196,12 +1196,15 @@ __device__ __forceinline__ void tile_of(const AttnParams &p, bool prefix, int x,
 // One launch for all of a call: the prefix's tiles, the tiles of requests of many rows, and the line of the others, whose reading of the
 // cache stands beside the tiles' products (three launches one after the other: prefix of 8011, 100 requests, 8-bit cache 94 us,
 // this 82; 40 mixed requests of D = 64 86 us, this 72).
-// Behind a prefix, both kinds are large, and as long as there are workgroups of both they take turns of one to a CU, so that a CU has one
-// of each: 256 requests of 10 to 2000 tokens behind 30000: 193 us with all tiles in front, 182 in turns.  Where a prefix's tile has at least
+// Where both kinds are large, behind a prefix or with a few prompts among many single tokens, they take turns of one to a CU as long as
+// there are workgroups of both, so that a CU has one of each: 256 requests of 10 to 2000 tokens behind 30000: 193 us with all tiles in front, 182 in turns.  Where a prefix's tile has at least
 // kLongPart blocks it goes first (256 requests behind 8000, 31 blocks: 70.5 us, the line first 75.1; behind 20000, 39 blocks: 134 and
 // 148), else the line (128 requests behind 8000, 15 blocks: 77.1 us, tiles first 87.5; 64 behind 16000, 15 blocks: 101 and 113).
-// Without a prefix all tiles go first (40 mixed requests: 71.3 us, in turns 74.4).
-constexpr int kTurn = 256, kLongPart = 24;
+// Without a prefix the largest request tells: with kFewLarge times the average's tokens (32 single tokens behind 4000 and a chunk of 512
+// behind 7500, 31 times: 139 us, with all tiles in front 172; 48 and 4 chunks of 300, D = 64, 13 times: 78 and 89; 64 and two prompts of
+// 1500, 32 times: 316 and 329) the tiles go first in turns, else all in front (60 requests of 1 to 300 tokens, 6 times: 83 us, in turns
+// 93; 12 of 1 to 1000, 7 times: 183 and 195; 16 single tokens and two chunks of 2000, 9 times: 207 and 215).
+constexpr int kTurn = 256, kLongPart = 24, kFewLarge = 12;
 template <int D, bool F8, bool TILES>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_kernel(AttnParams p)
 {
@@ -1443,8 +1446,9 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
     p.prefix_groups = p.prefix_blocks > 0 ? (unsigned)KVH * w.prefix_tiles * w.prefix_splits : 0u;
     p.tile_groups = wide ? KVH * (tiles + w.wide_parts) : 0u;
     const bool any_tiles = p.prefix_groups + p.tile_groups > 0;
-    p.turns = p.prefix_groups > 0 ? std::min(p.prefix_groups + p.tile_groups, (unsigned)(KVH * w.parts)) / kTurn : 0u;
-    p.tiles_first = p.prefix_groups > 0 && p.prefix_blocks / w.prefix_splits >= kLongPart;
+    const bool few_large = any_tiles && (int64_t)max_new * B >= (int64_t)kFewLarge * T;
+    p.turns = p.prefix_groups > 0 || few_large ? std::min(p.prefix_groups + p.tile_groups, (unsigned)(KVH * w.parts)) / kTurn : 0u;
+    p.tiles_first = p.prefix_groups == 0 || p.prefix_blocks / w.prefix_splits >= kLongPart;
     auto kernel = D == 128 ? (f8 ? (any_tiles ? attn_kernel<128, true, true> : attn_kernel<128, true, false>)
                                  : (any_tiles ? attn_kernel<128, false, true> : attn_kernel<128, false, false>))
                            : (f8 ? (any_tiles ? attn_kernel<64, true, true> : attn_kernel<64, true, false>)

@@ -115,6 +115,12 @@ def test_attention_of_long_contexts_and_prompts(lens, QH, KVH, D, ps, fp8, windo
     Case(lens, QH, KVH, D, ps, fp8, seed=1).check(window, sinks)
 
 
+def test_a_few_prompts_among_many_single_tokens():
+    # both kinds of workgroups, in turns: enough of each for a CU to have one
+    Case([(300 + i, 1) for i in range(40)] + [(90, 70)] + [(5, 1)] * 3, 16, 8, 64, 16, seed=19).check()
+    Case([(200, 1)] * 20 + [(700, 60)] + [(0, 0)] * 20, 32, 8, 64, 32, True, seed=20).check(window=150, sinks=3)
+
+
 def test_group_of_many_heads_and_a_large_batch():
     Case([(20, 2), (0, 1), (3, 0), (100, 5)], 256, 1, 64, 16, seed=2).check()
     Case([(i % 5, i % 3) for i in range(1024)], 2, 1, 64, 16, seed=3).check()
