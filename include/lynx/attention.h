@@ -90,8 +90,8 @@ int lynx_qk_norm_rope(const uint16_t *q, int64_t q_stride, const uint16_t *k, in
                       float v_scale, int num_pages, int page_size, void *stream);
 
 /* Bytes of device workspace that lynx_attention and lynx_attention_prefix need for these sizes (contents need not be
- * preserved; calls that share a workspace must not overlap in time).  prefix_len = 0 for lynx_attention.  The workspace
- * starts on 256 bytes. */
+ * preserved; calls that share a workspace must not overlap in time), 0 for sizes that they refuse.  prefix_len = 0 for
+ * lynx_attention.  The workspace starts on 256 bytes. */
 size_t lynx_attention_workspace_bytes(int B, int T, int QH, int KVH, int D, int prefix_len);
 
 /*

@@ -1469,7 +1469,9 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
 
 extern "C" size_t lynx_attention_workspace_bytes(int B, int T, int QH, int KVH, int D, int prefix_len)
 {
-    if (B <= 0 || T < 0 || QH <= 0 || KVH <= 0 || D <= 0 || prefix_len < 0) return 0;
+    if (B <= 0 || B > LYNX_MAX_REQUESTS || T < 0 || T > LYNX_MAX_STEP_TOKENS || KVH <= 0 || QH < KVH || QH > lynx::kMaxHeads || QH % KVH != 0 ||
+        QH / KVH > lynx::kMaxGroup || (D != 64 && D != 128) || prefix_len < 0)
+        return 0;
     return lynx::attention_space(T, QH / KVH, KVH, D, prefix_len).total;
 }
 

@@ -172,3 +172,11 @@ def test_scores_out_of_range_and_results_over_queries_are_refused():
         assert _attn(out=other, **kw) == -1 and b"scale * k_scale" in A.lib().lynx_last_error()
         assert _attn(prefix=True, out=other, **kw) == -1
     assert _attn(q=one, out=one) == -1 and b"out must not be q" in A.lib().lynx_last_error()
+
+
+def test_workspace_of_sizes_out_of_range_is_nothing():
+    # (sizes, some of which would be a division by zero or overflow an int on the way)
+    for sizes in ((4, 4, 2, 8, 128, 100), (4, 4, 6, 4, 128, 100), (1, 2 ** 31 - 1, 1024, 4, 128, 64), (1, 65537, 8, 8, 64, 64), (1, 1, 2 ** 31 - 1, 1, 64, 64),
+                  (1025, 4, 8, 2, 128, 64), (4, 4, 512, 1, 128, 64), (4, 4, 8, 2, 96, 64), (4, 4, 8, 0, 128, 64), (4, 4, -8, -2, 128, 64), (4, 4, 8, 2, 128, -1)):
+        assert L.attention_workspace_bytes(*sizes) == 0, sizes
+    assert L.attention_workspace_bytes(1024, 65536, 1024, 1024, 128, 2 ** 29) > L.attention_workspace_bytes(1024, 65536, 1024, 1024, 128) > 0
