@@ -11,7 +11,7 @@ from ctypes import c_float, c_int, c_int64, c_size_t, c_void_p
 import torch
 
 from . import binding
-from .binding import BF16, F32, I32, _check, _ptr, _stream
+from .binding import BF16, F32, I32, _check, _ptr
 
 ATTENTION_SYMBOLS = ["lynx_kv_assign", "lynx_qk_norm_rope", "lynx_attention_workspace_bytes", "lynx_attention", "lynx_attention_prefix"]
 MAX_REQUESTS, MAX_STEP_TOKENS, MAX_PAGES, MAX_PAGE_SIZE = 1024, 65536, 1048576, 1024
@@ -21,6 +21,7 @@ F64, FP8 = torch.float64, torch.float8_e4m3fn
 _FORMATS = {BF16: CACHE_BF16, FP8: CACHE_FP8}
 
 _lib = None
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)        # (its handle, as binding._stream has it)
 
 
 def lib():
@@ -43,7 +44,8 @@ def lib():
 
 
 # The host spends longer on these calls than the GPU does on a small batch, so every check is one pass over a tensor, and tensors that
-# a call has just allocated are not checked (lynx_kv_assign 17.7 -> 11.2 us of host time, lynx_qk_norm_rope 14.1 -> 12.0).
+# a call has just allocated are not checked (host time: lynx_kv_assign 17.7 -> 10.7 us, lynx_qk_norm_rope 14.1 -> 11.2; lynx_attention
+# takes 13.8, with two launches of 3.6 each).
 def _here(t, what):
     """The current device, on which kernels run; t: the call's first tensor."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -98,6 +100,13 @@ def _cache(k_cache, v_cache):
     return KVH, page_size, D, pages, fmt
 
 
+def _pages(k_cache, v_cache, here):
+    """Addresses of a cache whose sizes _cache has looked at."""
+    if k_cache.get_device() == here and v_cache.get_device() == here and k_cache.is_contiguous() and v_cache.is_contiguous():
+        return k_cache.data_ptr(), v_cache.data_ptr()
+    return _at(k_cache, k_cache.dtype, None, here, "k_cache"), _at(v_cache, v_cache.dtype, None, here, "v_cache")
+
+
 def new_cache(num_pages, KVH, page_size, D, dtype=BF16, device="cuda"):
     """(k_cache, v_cache) of one layer, uninitialised."""
     if dtype not in _FORMATS:
@@ -126,7 +135,7 @@ def lynx_kv_assign(ctx_len, new_len, T, page_size, block_table, free_ring, ring_
         made = [_at(out[n], I32, m, here, n) for n, m in zip(_ASSIGN_OUT, sizes)]
     _check(lib().lynx_kv_assign(_at(ctx_len, I32, B, here, "ctx_len"), _at(new_len, I32, B, here, "new_len"), B, T, page_size,
                                 free_ring.numel(), block_table.shape[1], shared_pages, _at(block_table, I32, None, here, "block_table"),
-                                _at(free_ring, I32, None, here, "free_ring"), _at(ring_state, I32, 2, here, "ring_state"), *made, _stream()))
+                                _at(free_ring, I32, None, here, "free_ring"), _at(ring_state, I32, 2, here, "ring_state"), *made, _current_stream(here)))
     return out
 
 
@@ -141,18 +150,18 @@ def lynx_qk_norm_rope(q, k, v, positions, slots, freqs, k_cache, v_cache, q_weig
     kp, ks = _rows(k, KVH, D, here, "k")
     vp, vs = _rows(v, KVH, D, here, "v")
     if q_out is None:
-        q_out = torch.empty(T, QH, D, dtype=BF16, device=q.device)
+        q_out = q.new_empty(T, QH, D)
         op, os_ = q_out.data_ptr(), QH * D
     else:
         op, os_ = _rows(q_out, QH, D, here, "q_out")
     if k.shape[0] != T or v.shape[0] != T or q_out.shape[0] != T:
         raise ValueError("q, k, v, q_out: the shapes do not match each other and the cache")
     rot = 0 if freqs is None else 2 * freqs.numel()
+    k_at, v_at = _pages(k_cache, v_cache, here)
     _check(lib().lynx_qk_norm_rope(qp, qs, kp, ks, vp, vs, _at(q_weight, BF16, D, here, "q_weight"), _at(k_weight, BF16, D, here, "k_weight"),
                                    eps, _at(positions, I32, T, here, "positions"), _at(slots, I32, T, here, "slots"),
                                    _at(freqs, F64, None, here, "freqs"), rot, 1 if interleaved else 0, T, QH, KVH, D, op, os_,
-                                   _at(k_cache, k_cache.dtype, None, here, "k_cache"), _at(v_cache, v_cache.dtype, None, here, "v_cache"), fmt,
-                                   k_scale, v_scale, pages, page_size, _stream()))
+                                   k_at, v_at, fmt, k_scale, v_scale, pages, page_size, _current_stream(here)))
     return q_out
 
 
@@ -174,7 +183,7 @@ def _attention(q, k_cache, v_cache, block_table, q_start, seq_len, max_new, scal
         raise ValueError("block_table: expected [requests, max_pages]")
     B, max_pages = block_table.shape
     if out is None:
-        out = torch.empty(T, QH, D, dtype=BF16, device=q.device)
+        out = q.new_empty(T, QH, D)
         op, os_ = out.data_ptr(), QH * D
     else:
         op, os_ = _rows(out, QH, D, here, "out")
@@ -182,7 +191,7 @@ def _attention(q, k_cache, v_cache, block_table, q_start, seq_len, max_new, scal
             raise ValueError("out: expected the shape of q")
     need = attention_workspace_bytes(B, T, QH, KVH, D, prefix[1] if prefix else 0)
     if workspace is None:
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+        workspace = q.new_empty(max(need, 256) // 2)         # (as bf16: need is a multiple of 256)
     elif workspace.get_device() != here or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
         raise ValueError(f"workspace: on {workspace.device}, {workspace.numel() * workspace.element_size()} bytes; needed {need} contiguous on cuda:{here}")
     if prefix:
@@ -190,10 +199,9 @@ def _attention(q, k_cache, v_cache, block_table, q_start, seq_len, max_new, scal
         prefix = (_at(prefix[0], I32, -(-prefix[1] // page_size), here, "prefix_table"), prefix[1])
     else:
         call = lib().lynx_attention
-    _check(call(qp, qs, _at(k_cache, k_cache.dtype, None, here, "k_cache"), _at(v_cache, v_cache.dtype, None, here, "v_cache"), fmt, k_scale, v_scale,
-                pages, page_size, _at(block_table, I32, None, here, "block_table"), max_pages, _at(q_start, I32, B + 1, here, "q_start"),
-                _at(seq_len, I32, B, here, "seq_len"), *prefix, B, T, max_new, QH, KVH, D, D ** -0.5 if scale is None else scale, *tail, op, os_,
-                _at(lse, F32, T * QH, here, "lse"), workspace.data_ptr(), _stream()))
+    _check(call(qp, qs, *_pages(k_cache, v_cache, here), fmt, k_scale, v_scale, pages, page_size, _at(block_table, I32, None, here, "block_table"),
+                max_pages, _at(q_start, I32, B + 1, here, "q_start"), _at(seq_len, I32, B, here, "seq_len"), *prefix, B, T, max_new, QH, KVH, D,
+                D ** -0.5 if scale is None else scale, *tail, op, os_, _at(lse, F32, T * QH, here, "lse"), workspace.data_ptr(), _current_stream(here)))
     return out
 
 
