@@ -171,6 +171,33 @@ def test_more_key_heads_than_the_line_has_workgroups():
     Case([(0, 1), (70, 2), (130, 1), (0, 0)], 520, 520, 64, 16, seed=14).check()
 
 
+@pytest.mark.parametrize("D,KVH,fp8", [(128, 1, False), (64, 2, True)])
+def test_the_largest_step(D, KVH, fp8):
+    # one prompt of 65536 tokens, the same as 1024 requests, and its second half behind the first as a shared prefix; and a few of its rows
+    # by themselves.  Each result is within 2^-8 (sum of weights times |v| + |result|) of the true one, as in the oracle's bound
+    T, QH, ps = 65536, 8, 256
+    g = torch.Generator(device="cuda").manual_seed(32)
+    kc, vc = L.new_cache(T // ps, KVH, ps, D, torch.float8_e4m3fn if fp8 else torch.bfloat16)
+    for c in (kc, vc):
+        c.copy_(torch.randn(c.shape, generator=g, device="cuda").to(c.dtype))
+    q = torch.randn(T, QH, D, generator=g, device="cuda").to(torch.bfloat16)
+    table = torch.randperm(T // ps, generator=g, device="cuda").to(torch.int32).view(1, -1)
+    biggest = float(vc.view(torch.uint8).view(vc.dtype).float().abs().max())
+    full = L.lynx_attention(q, kc, vc, table, i32([0, T]), i32([T]), T)
+
+    def same(part, lo):
+        want = full[lo:lo + part.shape[0]].float()
+        assert bool(((part.float() - want).abs() <= 2 * 1.02 * 2.0 ** -8 * (biggest + want.abs())).all())
+
+    for lo, n in ((0, 1), (0, 100), (16000, 1), (32000, 20), (65000, 536), (65535, 1), (40000, 300)):
+        same(L.lynx_attention(q[lo:lo + n].contiguous(), kc, vc, table, i32([0, n]), i32([lo + n]), n), lo)
+    starts, lengths = i32(list(range(0, T + 1, 64))), i32(list(range(64, T + 1, 64)))
+    rows = table.expand(1024, -1).contiguous()
+    same(L.lynx_attention(q, kc, vc, rows, starts, lengths, 64), 0)
+    half = T // 2
+    same(L.lynx_attention_prefix(q[half:], kc, vc, rows[512:].contiguous(), starts[:513], lengths[512:].contiguous(), 64, table[0, :half // ps].contiguous(), half), half)
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("n", [1, 40])
 def test_pages_behind_four_gib(fp8, n):
