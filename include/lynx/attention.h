@@ -8,11 +8,13 @@
  * hipGraph), LYNX_OK or a negative error with lynx_last_error(), nothing enqueued on error.  Inputs are assumed finite, except
  * that cache slots which no token occupies may hold anything.  No index array can cause an access out of bounds: tokens
  * whose page number lies outside [0, num_pages) are not written and not seen by any query, row ranges are clamped to [0, T], and
- * lengths to what a row of the block table can hold; what rows of out hold that lie in several requests' ranges is not specified.
+ * lengths to what a row of the block table can hold; what rows of out hold that lie in several requests' ranges, or in the range
+ * of a request whose q_start lies in front of an earlier one's, is not specified.
  *
  * A step: B requests, request b brings new_len[b] >= 0 new tokens behind the ctx_len[b] it has in the cache.  The T rows of q,
  * k, v, out, positions and slots hold the new tokens of request 0, then of request 1, and so on: request b's are rows
- * q_start[b] .. q_start[b+1]-1.  Rows behind the last request's are padding (a captured graph has a fixed T).
+ * q_start[b] .. q_start[b+1]-1.  Rows behind the last request's are padding (a captured graph has a fixed T), and so are rows in
+ * front of the first one's where q_start[0] > 0 (part of a larger step); the attention calls take padding rows that hold anything.
  *
  * Paged cache of one layer, page_size tokens a page (a multiple of 16), KVH key heads of D channels, elements bf16 or FP8 E4M3:
  *   k_cache [num_pages][KVH][page_size][D]    v_cache [num_pages][KVH][D][page_size]

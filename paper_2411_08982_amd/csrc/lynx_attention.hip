@@ -1311,7 +1311,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_finish_kernel(AttnParams p)
     }
     const unsigned long long what = line.what[lo];
     const int first = (int)(what >> 47), n = (int)(what >> 30 & 0x1ffffu), seq = (int)(what & 0x3fffffffu);
-    if (t >= first + n) return;
+    if (t < first || t >= first + n) return;        // (rows in front of the first request's are nobody's either)
     const bool behind = behind_prefix(p, seq - n);
     const int own_row = (t - first) * p.G + head % p.G;
     float m = -INFINITY, l = 0.0f;
