@@ -75,7 +75,8 @@ int lynx_kv_assign(const int32_t *ctx_len, const int32_t *new_len, int B, int T,
  *   the first `rot` channels, pairs (a, b) = (y[i], y[i + rot/2]) or, interleaved, (y[2i], y[2i+1]):
  *     a' = a cos(phi) - b sin(phi),  b' = b cos(phi) + a sin(phi),  phi = positions[t] * freqs[i],
  *   channels from rot on pass.  The product is taken and reduced to one turn in fp64, so far positions lose nothing.  One rounding
- *   to bf16 (or to E4M3 after the division by its scale, magnitudes beyond 448 to 448) at the end.
+ *   to bf16 (or to E4M3 after the division by its scale, magnitudes beyond 448 to 448) at the end.  A NaN in k or v stays one in
+ *   either cache.
  *   q [T][QH][D], k, v [T][KVH][D] bf16; q_stride, k_stride, v_stride = elements from one token to the next (heads of a token are
  *   contiguous), so that q, k, v can be parts of one row of a fused projection.  q_weight, k_weight [D] bf16 or NULL.
  *   freqs [rot/2] fp64, radians per position; rot = 0 (freqs may be NULL) rotates nothing.

@@ -200,7 +200,8 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8])
     return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
 }
 
-__device__ __forceinline__ float in_e4m3_range(float x) { return fminf(fmaxf(x, -448.0f), 448.0f); }
+// (by comparisons: what is no number stays none, as in a bf16 cache; fmaxf and fminf would make it -448)
+__device__ __forceinline__ float in_e4m3_range(float x) { return x > 448.0f ? 448.0f : x < -448.0f ? -448.0f : x; }
 
 __device__ __forceinline__ uint2 pack8_fp8(const float (&x)[8], float scale)
 {
