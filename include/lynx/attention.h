@@ -51,7 +51,8 @@ extern "C" {
  *   taken from the free ones and never given back (a request that starts on a shared prefix has ctx_len = its length).
  *   free_ring [num_pages] int32, in and out, and ring_state [2] int32 = {head, count}: the free pages are the count entries from
  *   place head on, round the ring.  New pages are taken at the head, in request order and token order; pages of ended requests
- *   are put behind the last free one, in the same orders, and are not given out again by the same call.
+ *   are put behind the last free one, in the same orders, and are not given out again by the same call.  A head or count outside
+ *   the ring is brought into it: the head modulo num_pages, the count to 0 .. num_pages.
  *   q_start [B+1] int32 out; seq_len [B] int32 out = ctx_len + new_len (0 for an ended request); positions [T] int32 out =
  *   place of the token in its sequence, 0 in padding rows; slots [T] int32 out, -1 in padding rows and for pages outside the
  *   cache; ring_state_out [2] int32 out.  seq_len may be ctx_len and ring_state_out may be ring_state, so that a captured
@@ -60,11 +61,15 @@ extern "C" {
  *     LYNX_KV_NO_PAGES   the free pages did not suffice: the first request that they do not cover, and all behind it that bring
  *                        tokens, get none (they keep ctx_len, bring no rows and can be tried again);
  *     LYNX_KV_NO_ROWS    the same for the T rows;
- *     LYNX_KV_TOO_LONG   a request does not fit its row of the block table, or has a negative length: it alone is passed over.
+ *     LYNX_KV_TOO_LONG   a request does not fit its row of the block table, or has a negative length: it alone is passed over;
+ *     LYNX_KV_LOST_PAGES the ring has no place for all pages of the ended requests, which no pool of num_pages pages comes to whose
+ *                        pages are each in one place (a count that is wrong, a page in two rows, shared_pages smaller than when
+ *                        the rows were filled): as many as there is place for were put back, in order, the others are lost.
  */
 #define LYNX_KV_NO_PAGES 1
 #define LYNX_KV_NO_ROWS 2
 #define LYNX_KV_TOO_LONG 4
+#define LYNX_KV_LOST_PAGES 8
 int lynx_kv_assign(const int32_t *ctx_len, const int32_t *new_len, int B, int T, int page_size, int num_pages, int max_pages,
                    int shared_pages, int32_t *block_table, int32_t *free_ring, const int32_t *ring_state, int32_t *q_start,
                    int32_t *seq_len, int32_t *positions, int32_t *slots, int32_t *ring_state_out, int32_t *status, void *stream);

@@ -15,7 +15,7 @@ from .binding import BF16, F32, I32, _check, _ptr
 
 ATTENTION_SYMBOLS = ["lynx_kv_assign", "lynx_qk_norm_rope", "lynx_attention_workspace_bytes", "lynx_attention", "lynx_attention_prefix"]
 MAX_REQUESTS, MAX_STEP_TOKENS, MAX_PAGES, MAX_PAGE_SIZE = 1024, 65536, 1048576, 1024
-KV_NO_PAGES, KV_NO_ROWS, KV_TOO_LONG = 1, 2, 4
+KV_NO_PAGES, KV_NO_ROWS, KV_TOO_LONG, KV_LOST_PAGES = 1, 2, 4, 8
 CACHE_BF16, CACHE_FP8 = 0, 1
 F64, FP8 = torch.float64, torch.float8_e4m3fn
 _FORMATS = {BF16: CACHE_BF16, FP8: CACHE_FP8}

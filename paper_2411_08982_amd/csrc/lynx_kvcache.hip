@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kAssignThreads) void assign_kernel(AssignParams p)
         const int held = (ctx + p.page_size - 1) / p.page_size;
         have = max(held, p.shared_pages);
         take = min(max((ctx + n + p.page_size - 1) / p.page_size - have, 0), p.num_pages + 1);
-        back = ended ? min(max(held - p.shared_pages, 0), p.num_pages) : 0;
+        back = ended ? min(max(held - p.shared_pages, 0), p.num_pages + 1) : 0;
     }
     int v[3] = {min(n, p.T + 1), take, back};    // (bounded, so that 1024 of them stay below 2^31)
     scan3(sh, v);
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(kAssignThreads) void assign_kernel(AssignParams p)
     if (b == 0) {
         p.ring_state_out[0] = (head + fresh) % p.num_pages;
         p.ring_state_out[1] = count - fresh + returned;
-        *p.status = sh.status;
+        *p.status = sh.status | (sh.back_end[p.B - 1] > returned ? LYNX_KV_LOST_PAGES : 0);
     }
     if (p.tokens_apart) return;
     __syncthreads();   // the new entries of the block table
