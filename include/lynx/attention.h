@@ -99,7 +99,10 @@ int lynx_qk_norm_rope(const uint16_t *q, int64_t q_stride, const uint16_t *k, in
 
 /* Bytes of device workspace that lynx_attention and lynx_attention_prefix need for these sizes (contents need not be
  * preserved; calls that share a workspace must not overlap in time), 0 for sizes that they refuse.  prefix_len = 0 for
- * lynx_attention.  The workspace starts on 256 bytes. */
+ * lynx_attention.  The workspace starts on 256 bytes.  The size does not fall when B, T or prefix_len grows: a workspace for the
+ * largest step serves all smaller ones.  lynx_attention: about 288 * max(512, KVH) * (D + 2) * 4 bytes, 77 MB for D = 128 and up to 512 key
+ * heads.  A prefix adds about 2 * R * KVH * (D + 2) * 4 bytes, R = min(T * QH / KVH, 128 * B, B * prefix_len / 4); where R * KVH is less than 65536,
+ * the half of it for the prefix's own parts may be up to what 65536 takes (34 MB for D = 128). */
 size_t lynx_attention_workspace_bytes(int B, int T, int QH, int KVH, int D, int prefix_len);
 
 /*
@@ -128,6 +131,8 @@ int lynx_attention(const uint16_t *q, int64_t q_stride, const void *k_cache, con
  *   page is copied into each request's own page there).
  *   prefix_len (host) >= 0, <= max_pages * page_size; it need not be a multiple of anything.  Rows at positions inside the
  *   prefix see what is up to them, as in lynx_attention.
+ *   Where that would not pay, T * QH / KVH >= 128 * B or > B * prefix_len / 4 (prompt chunks, whose rows fill the matrix products by
+ *   themselves; a prefix that is short against them), the prefix is read through block_table, too, and the workspace is lynx_attention's.
  */
 int lynx_attention_prefix(const uint16_t *q, int64_t q_stride, const void *k_cache, const void *v_cache, int cache_format,
                           float k_scale, float v_scale, int num_pages, int page_size, const int32_t *block_table, int max_pages,

@@ -1359,10 +1359,22 @@ inline int narrow_rows(bool f8) { return f8 ? 2 * kRows : kRows; }
 // parts fewer than twice wide_parts, and such tiles at most wide_parts.
 // The prefix's tiles leave every row's parts, and the rows behind the prefix their own.
 struct AttnSpace {
-    int parts, wide_parts, prefix_tiles, prefix_splits;
+    int parts, wide_parts, prefix_blocks, prefix_tiles, prefix_splits;
     size_t ml_off, cuts_off, wide_o_off, wide_ml_off, prefix_o_off, prefix_ml_off, own_o_off, own_ml_off, total;
 };
-static AttnSpace attention_space(int T, int G, int KVH, int D, int prefix_len)
+// Whether a shared prefix is read apart.  Each row then leaves its own part and the prefix's, unnormalised and in fp32, in the workspace, which
+// are written and read again.  A request whose rows fill a tile of 128 gains nothing by it, since the tiles read the prefix for 128 rows
+// either way (8 key heads of 4 query heads, 64 requests of 128 rows and 200 tokens of their own: behind 64 tokens 37 us through the block table
+// and apart 67, behind 1024 65 and 94, behind 16384 554 and 570; 16 of 96 rows behind 16384 the other way round, 151 and 134), nor does one
+// whose rows are many against the prefix (64 requests of 32 rows, 4 key heads, behind 64 tokens: 21.2 and 30.1; behind 256, 8 tokens
+// for a row, 25.1 and 30.4; behind 1024, 32, 41.6 and 36.0).
+constexpr int kApart = 4;               // tokens of the prefix for each row of a request
+inline bool reads_apart(int B, int T, int G, int prefix_len)
+{
+    const int64_t rows = (int64_t)T * G;            // of all requests for a key head
+    return rows < (int64_t)B * kTileRows && rows * kApart <= (int64_t)B * prefix_len;
+}
+static AttnSpace attention_space(int B, int T, int G, int KVH, int D, int prefix_len)
 {
     AttnSpace w;
     w.parts = kWorkgroups / KVH > 0 ? kWorkgroups / KVH : 1;
@@ -1380,20 +1392,26 @@ static AttnSpace attention_space(int T, int G, int KVH, int D, int prefix_len)
     // 16000, 15 blocks: 95 and 85; 64 behind 16000, 8 blocks: 121 and 101; 256 behind 16000, 31 blocks: 109 and 111, with 2000 tokens
     // of their own 213 and 208; behind 30000, 58 blocks: 173 and 186.  100 requests of 2 to 5 tokens behind 8011, whose 88 tiles
     // fill two thirds of one half: 78 and 94.
-    const int blocks = prefix_len / kBlock;
+    const int blocks = T > 0 && reads_apart(B, T, G, prefix_len) ? prefix_len / kBlock : 0;
+    w.prefix_blocks = blocks;
     w.prefix_tiles = (int)(((int64_t)T * G + kTileRows - 1) / kTileRows);
     const int tiles = w.prefix_tiles * KVH;
     w.prefix_splits = 0;
-    if (blocks > 0 && T > 0) {
+    if (blocks > 0) {
         int splits = std::max(1, kWorkgroups / tiles);
         const int half = kWorkgroups / 2 / tiles;
         if (blocks / splits < 32 && half * tiles * 8 >= kWorkgroups / 2 * 7) splits = half;
         w.prefix_splits = std::min(splits, (blocks + 3) / 4);
     }
-    const size_t prefix_rows = (size_t)w.prefix_tiles * w.prefix_splits * KVH * kTileRows;
+    // Room for what any step of at most these sizes needs, so that a workspace for the largest one serves all: the most rows for which the
+    // prefix may be read apart, and the most parts that they are cut into.
+    const int64_t all_blocks = prefix_len / kBlock;
+    const int64_t most = all_blocks > 0 ? std::min(std::min((int64_t)T * G, (int64_t)B * kTileRows - 1), (int64_t)B * prefix_len / kApart) : 0;
+    const int64_t most_tiles = (most + kTileRows - 1) / kTileRows * KVH;
+    const size_t prefix_rows = (size_t)std::max(most_tiles, std::min<int64_t>(kWorkgroups, most_tiles * ((all_blocks + 3) / 4))) * kTileRows;
     w.prefix_ml_off = w.prefix_o_off + align256(prefix_rows * D * 4);
     w.own_o_off = w.prefix_ml_off + align256(prefix_rows * 8);
-    const size_t own_rows = w.prefix_splits > 0 ? (size_t)T * G * KVH : 0;
+    const size_t own_rows = (size_t)most * KVH;
     w.own_ml_off = w.own_o_off + align256(own_rows * D * 4);
     w.total = w.own_ml_off + align256(own_rows * 8);
     return w;
@@ -1428,7 +1446,7 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
     if (out == q) return fail(LYNX_ERR_INVALID_ARG, "%s: out must not be q", who);
     if (((uintptr_t)workspace & 255) != 0) return fail(LYNX_ERR_INVALID_ARG, "%s: the workspace must start on 256 bytes", who);
     const int G = QH / KVH;
-    const AttnSpace w = attention_space(T, G, KVH, D, prefix_len);
+    const AttnSpace w = attention_space(B, T, G, KVH, D, prefix_len);
     const int narrow = narrow_rows(cache_format == LYNX_CACHE_FP8);
     const bool wide = (int64_t)T * G > narrow && (int64_t)max_new * G > narrow;
     char *const ws = (char *)workspace;
@@ -1436,7 +1454,7 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
                     num_pages, max_pages, page_size, page_multiplier(page_size), reciprocal(G), reciprocal(w.parts), scale2, v_scale,
                     window < kMaxContext ? window : 0, sinks < kMaxContext ? sinks : kMaxContext,   // (a window that long hides nothing)
                     w.parts, (float *)ws, (float *)(ws + w.ml_off), (Cut *)(ws + w.cuts_off), wide ? narrow : INT_MAX, w.wide_parts, (float *)(ws + w.wide_o_off),
-                    (float *)(ws + w.wide_ml_off), prefix_len / kBlock, w.prefix_splits, (float *)(ws + w.prefix_o_off), (float *)(ws + w.prefix_ml_off),
+                    (float *)(ws + w.wide_ml_off), w.prefix_blocks, w.prefix_splits, (float *)(ws + w.prefix_o_off), (float *)(ws + w.prefix_ml_off),
                     (float *)(ws + w.own_o_off), (float *)(ws + w.own_ml_off)};
     const bool f8 = cache_format == LYNX_CACHE_FP8;
     const dim3 threads(kAttnThreads);
@@ -1472,7 +1490,7 @@ extern "C" size_t lynx_attention_workspace_bytes(int B, int T, int QH, int KVH, 
     if (B <= 0 || B > LYNX_MAX_REQUESTS || T < 0 || T > LYNX_MAX_STEP_TOKENS || KVH <= 0 || QH < KVH || QH > lynx::kMaxHeads || QH % KVH != 0 ||
         QH / KVH > lynx::kMaxGroup || (D != 64 && D != 128) || prefix_len < 0)
         return 0;
-    return lynx::attention_space(T, QH / KVH, KVH, D, prefix_len).total;
+    return lynx::attention_space(B, T, QH / KVH, KVH, D, prefix_len).total;
 }
 
 extern "C" int lynx_attention(const uint16_t *q, int64_t q_stride, const void *k_cache, const void *v_cache, int cache_format,
