@@ -6,7 +6,8 @@ aligned to kStageAlign and the kernel's other arrays are smaller than that toget
 the buffers moves the end of the segment by a whole kStageAlign, and the segment's size shows it.
 
 The attention kernel's four LDS buffers for blocks of the cache are filled by such loads too: aligned to ATTENTION_ALIGN, which is more
-than the kernel's other arrays take together.
+than the kernel's other arrays take together.  Its tiles wait at barriers, as below.  Its waves of few rows have four units of a block on their way
+and read each behind a wait that leaves as many loads outstanding as come behind that unit: check_units counts them in the machine code.
 
 Waits: a wave reports its pieces of a chunk of token rows at a barrier, before which they must have landed.  The kernel waits
 until at most as many loads are outstanding as it has issued behind them, a number that follows from its source as long as
@@ -84,7 +85,7 @@ def check_waits(listing: str) -> int:
             name, behind = head.group(1), None
             continue
         words = line.split("//")[0].split()
-        if not words or KERNEL not in name:
+        if not words or (KERNEL not in name and ATTENTION not in name):
             continue
         op = words[0]
         if op.startswith(("buffer_", "global_", "flat_", "scratch_")):
@@ -101,6 +102,77 @@ def check_waits(listing: str) -> int:
             barriers += 1
             behind = None
     return barriers
+
+
+UNITS = 4             # units of a block that a wave has on their way
+
+
+def check_units(listing: str) -> int:
+    """Raises if a wave of the attention kernel can read a unit of a block from LDS before all loads of it have landed; the number of
+    units read.
+
+    The loads are followed in the order of the listing: the first run of them is UNITS units, each wait that reads follow is for the
+    oldest unit, and behind each unit read come the loads of another or, in a tile's last block, none.  A branch has to find as many
+    loads on their way as its target does in that order, which then stands for every path."""
+    read = 0
+    name, start = "", 0
+    unit = 0              # loads of a unit
+    out = []              # memory operations on their way, oldest first; True: a load into LDS
+    waited = None         # the last wait's count, None: reads have followed it
+    at = {}               # address -> loads on their way there, by the listing or by a branch ahead of it
+
+    def fail(what):
+        raise RuntimeError(f"{name}: {what}")
+
+    def whole_units():
+        if sum(out) % unit:
+            fail(f"{sum(out)} loads into LDS on their way, in units of {unit}")
+        return sum(out) // unit
+
+    for line in listing.splitlines():
+        head = re.match(r"([0-9a-f]+) <(\S+)>:", line)
+        if head:
+            if out:
+                fail("loads into LDS on their way at its end")
+            start, name, unit, waited, at = int(head.group(1), 16), head.group(2), 0, None, {}
+            continue
+        words = line.split("//")[0].split()
+        if not words or ATTENTION not in name:
+            continue
+        op, address = words[0], re.search(r"//\s*([0-9A-Fa-f]+):", line)
+        if op.startswith("global_load_lds"):
+            out.append(True)
+        elif not out:
+            continue
+        elif op.startswith(("buffer_", "global_", "flat_", "scratch_")):
+            out.append(False)
+        elif op == "s_waitcnt" and "vmcnt" in line:
+            if unit == 0:
+                unit = sum(out) // UNITS
+                if unit == 0 or whole_units() != UNITS:
+                    fail(f"{sum(out)} loads into LDS ahead of the first wait, not {UNITS} units")
+            waited = int(re.search(r"vmcnt\((\d+)\)", line).group(1))
+        elif op.startswith("ds_read") and waited is not None:
+            whole_units()
+            oldest = [i for i, lds in enumerate(out) if lds][unit - 1]
+            if waited > len(out) - 1 - oldest:
+                fail(f"a unit is read with {waited} loads outstanding, {len(out) - 1 - oldest} behind it")
+            del out[:oldest + 1]
+            read, waited = read + 1, None
+            if not any(out):
+                out, unit = [], 0
+        elif op.startswith("ds_read") and unit == 0:
+            fail("a unit is read without a wait")
+        places = [int(address.group(1), 16)] if address else []
+        jump = re.search(r"<\S+?(?:\+0x([0-9a-f]+))?>\s*$", line) if op.startswith(("s_branch", "s_cbranch")) else None
+        if jump:
+            places.append(start + int(jump.group(1) or "0", 16))
+        for place in places:
+            if at.setdefault(place, sum(out)) != sum(out):
+                fail(f"{sum(out)} and {at[place]} loads into LDS on their way at {place:#x}")
+    if out:
+        fail("loads into LDS on their way at its end")
+    return read
 
 
 SUM_STATES = 19       # most wait states between a product and another instruction on its sums
@@ -199,11 +271,12 @@ def check_operands(listing: str) -> int:
 
 
 def check(lib_path: str) -> None:
-    kernels = barriers = products = attention = 0
+    kernels = barriers = products = attention = units = 0
     for notes, listing in code_object_texts(lib_path):
         kernels += check_placement(notes)
         barriers += check_waits(listing)
         products += check_operands(listing)
         attention += check_attention_placement(notes)
-    if kernels == 0 or barriers < kernels or products == 0 or attention == 0:
-        raise RuntimeError(f"{lib_path}: {kernels} kernels, {barriers} barriers, {products} products and {attention} attention kernels found: the checks do not read this library")
+        units += check_units(listing)
+    if kernels == 0 or barriers < kernels or products == 0 or attention == 0 or units < attention:
+        raise RuntimeError(f"{lib_path}: {kernels} kernels, {barriers} barriers, {products} products, {attention} attention kernels and {units} of their units found: the checks do not read this library")
