@@ -39,6 +39,7 @@ struct AttnParams {
     unsigned page_mul;                  // division of a group of 16 tokens by the page size: page_of
     unsigned group_mul, parts_mul;      // division of rows by G (token_of) and of the line by parts (length_of)
     float scale2, v_scale;              // scale * k_scale * log2 e
+    float lag;                          // 8 / scale2: by how much the maximum of a tile's row may fall behind
     int window, sinks;
     int parts;                          // parts that the contexts of all tiles together are cut into, per key head
     float *part_o, *part_ml;            // workspace: unfinished rows
@@ -1024,7 +1025,9 @@ __device__ __forceinline__ void tile_of(const AttnParams &p, bool prefix, int x,
         if (real) u = *reinterpret_cast<const u32x4 *>(p.q + (size_t)(first + tok) * p.q_stride + (size_t)head * D + i * 16 + hf * 8);
         q[i] = __builtin_bit_cast(bf16x8, u);
     }
-    float m = -INFINITY, l = 0.0f;
+    float m = -INFINITY, l = 0.0f;                  // (m: of the scores themselves)
+    constexpr float kFarScore = 1048576.0f;
+    bool far = false;                               // whether a row's maximum is beyond it
     f32x16 o[NV];
 #pragma unroll
     for (int t = 0; t < NV; ++t)
@@ -1137,16 +1140,27 @@ __device__ __forceinline__ void tile_of(const AttnParams &p, bool prefix, int x,
             for (int j = 0; j < 16; ++j) top = fmaxf(top, z[t][j]);
 #pragma unroll
         for (int j = 0; j < kBefore; ++j) first_product(j);
-        top = half_max(top) * p.scale2;
-        // m follows the maximum only when it is 8 behind: until then weights are up to 2^8, and rows are rescaled less often
-        if (__any(top > m + 8.0f)) {
-            const float up = fmaxf(m, top), a = up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - up);
+        top = half_max(top);
+        // m follows the maximum only when it is 8 behind, times the scale: until then weights are up to 2^8, and rows are rescaled less often
+        if (__any(top > m + p.lag)) {
+            const float up = fmaxf(m, top), a = up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - up) * p.scale2);
             l *= a;
 #pragma unroll
             for (int t = 0; t < NV; ++t) o[t] *= a;
             m = up;
+            far = __any(m != -INFINITY && fabsf(m * p.scale2) > kFarScore);
         }
-        const float off = m == -INFINITY ? 0.0f : -m;
+        // 2^(z scale - m scale) by one multiply-add.  The product with m is rounded, which moves all weights of a row by as much; where that could be
+        // by more than 2^(1/32), and with larger scores out of range, m is taken off the scores first.
+        float off = m == -INFINITY ? 0.0f : -m * p.scale2;
+        if (far) {
+            const float by = fabsf(off) > kFarScore ? m : 0.0f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) z[t][j] -= by;
+            off = by == 0.0f ? off : 0.0f;
+        }
 #pragma unroll
         for (int j = kBefore; j < 2 * NQ; ++j) first_product(j);
 #pragma unroll
@@ -1175,6 +1189,7 @@ __device__ __forceinline__ void tile_of(const AttnParams &p, bool prefix, int x,
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // nothing on its way into LDS when the workgroup ends
     l = half_sum(l);
+    m *= p.scale2;
     if (!real) return;
     // lane: channels 32 t + 8 j + 4 hf .. + 3 of its row
     f32x4 c[D / 8];
@@ -1452,6 +1467,7 @@ static int attention_impl(const char *who, const uint16_t *q, int64_t q_stride, 
     char *const ws = (char *)workspace;
     AttnParams p = {q, k_cache, v_cache, block_table, q_start, seq_len, prefix_table, out, lse, q_stride, out_stride, B, T, KVH, G,
                     num_pages, max_pages, page_size, page_multiplier(page_size), reciprocal(G), reciprocal(w.parts), scale2, v_scale,
+                    std::min(8.0f / scale2, FLT_MAX),
                     window < kMaxContext ? window : 0, sinks < kMaxContext ? sinks : kMaxContext,   // (a window that long hides nothing)
                     w.parts, (float *)ws, (float *)(ws + w.ml_off), (Cut *)(ws + w.cuts_off), wide ? narrow : INT_MAX, w.wide_parts, (float *)(ws + w.wide_o_off),
                     (float *)(ws + w.wide_ml_off), w.prefix_blocks, w.prefix_splits, (float *)(ws + w.prefix_o_off), (float *)(ws + w.prefix_ml_off),
