@@ -115,7 +115,7 @@ size_t lynx_attention_workspace_bytes(int B, int T, int QH, int KVH, int D, int 
  * product (their sum is taken before the rounding).  The new tokens' keys and values are in the cache already.
  *   max_new (host): the largest number of new tokens of a request, as far as the caller knows it (1 for a pure decode batch);
  *   which kernels are launched goes by it, the result does not depend on it being right.
- *   scale > 0, scale * k_scale a normal float; window, sinks >= 0.  q_stride, out_stride as in lynx_qk_norm_rope (lse is dense); out does
+ *   scale > 0, scale * k_scale a normal float; scores, q . k and times scale * k_scale * log2 e, within a float's range; window, sinks >= 0.  q_stride, out_stride as in lynx_qk_norm_rope (lse is dense); out does
  *   not overlap q (a row is read by several workgroups).
  */
 int lynx_attention(const uint16_t *q, int64_t q_stride, const void *k_cache, const void *v_cache, int cache_format,

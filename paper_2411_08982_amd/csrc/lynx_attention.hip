@@ -540,8 +540,9 @@ struct alignas(16) Cut {
 // LDS, and when all waves are through, the parts of each tile are joined: to the finished rows, or to a part in the workspace if
 // the tile goes on in another workgroup.  (With all four waves on one tile after the other, each with its round trips for lengths,
 // queries and page numbers, 256 requests with an 8-bit cache took 137 us where this took 118.)
-// Bound by HBM: 64 requests of 500 to 12000 tokens, 411 MB: 69 us, 6.0 TB/s; 256 with 657 MB of 8-bit cache: 118 us, 5.6 TB/s; a plain
-// read of such pages reaches 6.0, with the hint 6.6.  One request of 9001 tokens: 11.4 us, four dependent trips to memory.
+// Bound by HBM: 64 requests of 500 to 12000 tokens, 411 MB: 72 us, 5.7 TB/s; 256 with 657 MB of 8-bit cache: 127 us, 5.2 TB/s; a plain
+// read of such pages reaches 6.0, with the hint 6.6.  One request of 9001 tokens: 12.0 us, four dependent trips to memory.  (Medians of
+// a kernel trace, as all times of whole kernels here.)
 constexpr int kRecords = 2 * kAttnWaves;
 struct RowsShared {
     Line line;
@@ -748,13 +749,18 @@ __device__ __forceinline__ void join_rows(const AttnParams &p, unsigned cut_inde
 // two buffers, and every fragment that a wave reads there serves 32 rows.  The same transposed products as above: a lane has row
 // l % 32, and a result fragment of S^T gives it 16 tokens of a block's half; the keys lie in LDS in such an order that they are two
 // runs of 8 consecutive tokens, the operand of the second product.
-// What bounds it: per block and wave 32 matrix instructions (1024 cycles; D = 64: 512), 32 KiB from LDS (four waves: 1024 cycles of its
+// What it does: per block and wave 32 matrix instructions (1024 cycles; D = 64: 512), 32 KiB from LDS (four waves: 1024 cycles of its
 // 128 bytes each) and about 900 VALU cycles for 32 weights per lane, 512 of them exponentials; two workgroups a CU, so that one's
-// softmax stands beside the other's products.  Five prompt chunks of 700 to 2048 tokens, 236 GFLOP: 266 us, 890 TFLOP/s, matrix cores
-// and VALU 46 % busy each; with D = 64 it is the VALU's work (40 requests, 22 GFLOP: 72 us).
+// softmax can stand beside the other's products.  Five prompt chunks of 700 to 2048 tokens, 236 GFLOP: 294 us, 804 TFLOP/s (265 us, 890, where
+// no profiler runs).  None of the three is full, matrix cores, VALU and LDS 46 % each: the two workgroups mostly take turns, and in the second
+// copy of the loop's turn the compiler has most exponentials in front of the last products.  With D = 64 (40 requests, 22 GFLOP: 75 us;
+// VALU 48 %, matrix cores 19 %) tiles are short, 6.5 blocks behind a start of 4 us, and are dealt out in the requests' order, so that a long one may
+// begin last.
 constexpr int kWaveRows = 32;
 constexpr int kLdsAlign = 16384, kBuffer = kLdsAlign / 16;      // bytes and 16-byte pieces of each of the four buffers in LDS
-constexpr int kMinChunk = 8;                // blocks: a part of a tile's context is not made shorter (one request of 3000 tokens, 100 of them new: 33.0 us, with 4 34.7, with 16 39.3)
+// Blocks: what a request's first and last row see together is not cut into shorter parts (one request of 3000 tokens, 100 of them new: 33.0 us,
+// with 4 34.7, with 16 39.3).  Of a long prompt with a short window a tile sees less than that, and its parts are shorter.
+constexpr int kMinChunk = 8;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // The contexts of all tiles are cut into parts of at most `chunk` blocks, chunk following from the work of the whole batch, so that a
@@ -1307,7 +1313,8 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnParams p, u
 
 // What is left behind a call with a shared prefix: a row behind the prefix is joined from the prefix's parts and its own, and where the
 // row's tile of 16 is cut, from that tile's parts, which join_rows would join first (its launch, of 5 us, is saved).  D / 4 lanes to a
-// row, rows in the order of out.  Bound by the parts' bytes (256 requests, 8 parts, 33 MB: 10.8 us), with few rows by latency (12: 5.4).
+// row, rows in the order of out.  256 requests, 8192 rows, 33 MB of parts: 11.7 us; 100 requests, 11000 rows: 9.8, of which the sums of all requests'
+// lengths, which each workgroup takes for itself, are a good part; with few rows latency (12: 5.6).
 template <int D>
 __global__ __launch_bounds__(kAttnThreads) void attn_finish_kernel(AttnParams p)
 {

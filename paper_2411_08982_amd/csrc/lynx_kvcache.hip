@@ -7,8 +7,8 @@ namespace lynx {
 // ---- lynx_kv_assign ---------------------------------------------------------------------------------------------------
 // Prefix sums over at most 1024 requests say where each request's rows, new pages and returned pages begin; then every new
 // page, returned page and token finds its request by bisection in the sums.  Nothing here is bound by bytes: one workgroup,
-// one thread per request, and what counts is the number of round trips (64 requests of one token: 4.2 us; 1000 of 1 to 60: 5.2 us and
-// 4.1 for the tokens).
+// one thread per request, and what counts is the number of round trips (64 requests of one token: 4.3 us; 1000 of 1 to 60: 5.3 us and
+// 4.0 for the tokens).
 constexpr int kAssignThreads = LYNX_MAX_REQUESTS;
 // More tokens are left to a launch of their own (64 requests: 2048 tokens 5.7 us here, 6.5 apart; 4096 7.3 and 6.7; 8192 10.6 and 6.6).
 constexpr int kTokensHere = 2048;
@@ -166,7 +166,8 @@ __global__ __launch_bounds__(kTokenThreads) void assign_tokens_kernel(AssignPara
 // heads and computed once, into LDS; a head row is held by D/8 lanes, 8 channels (16 bytes) each.  The others turn 32 tokens' values
 // of one key head over in LDS, since the cache has them transposed: where the tokens' slots follow one another, as a prompt's do, a
 // channel's run of 16 bytes is one store.  (Element by element 8001 tokens with 8 key heads took 70 us, with 16 of 16 heads 141.)
-// Bound by HBM: 8001 tokens, 32 query and 8 key heads, 197 MB: 38.9 us, 5.1 TB/s; 32 tokens: 5.3 us of latency.
+// Bound by HBM: 8001 tokens, 32 query and 8 key heads, 197 MB: 39.2 us, 5.0 TB/s; with an 8-bit cache 180 MB: 43.8 us, 4.1 TB/s (its conversions,
+// and its runs take 16 tokens); 32 tokens: 5.4 and 5.6 us of latency.
 constexpr int kRopeThreads = 256;
 // More at a time lose fewer runs at their borders, fewer have more workgroups (8 key heads; prompts that begin off a page: 8000 tokens
 // 35.4 us by 32, by 16 37.7, by 64 36.3; 256 tokens 5.2 by 32, 4.7 by 16, 6.4 by 64).
