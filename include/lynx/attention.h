@@ -132,7 +132,7 @@ int lynx_attention(const uint16_t *q, int64_t q_stride, const void *k_cache, con
  *   prefix_len (host) >= 0, <= max_pages * page_size; it need not be a multiple of anything.  Rows at positions inside the
  *   prefix see what is up to them, as in lynx_attention.
  *   Where that would not pay, T * QH / KVH >= 128 * B or > B * prefix_len / 4 (prompt chunks, whose rows fill the matrix products by
- *   themselves; a prefix that is short against them), the prefix is read through block_table, too, and the workspace is lynx_attention's.
+ *   themselves; a prefix that is short against them), the prefix is read through block_table, too, as lynx_attention does.
  */
 int lynx_attention_prefix(const uint16_t *q, int64_t q_stride, const void *k_cache, const void *v_cache, int cache_format,
                           float k_scale, float v_scale, int num_pages, int page_size, const int32_t *block_table, int max_pages,
